@@ -269,6 +269,78 @@ int moe_combine(const moe_problem_t *p, const void *staging, const uint32_t *fla
                 void *stream);
 
 /*
+ * Training the layer around a program's own expert products: gate, dispatch, g = x_perm W1 and u = x_perm W3 (the
+ * program), moe_swiglu, y = h W2 (the program), moe_unsort; and back: moe_unsort_backward, the program's products,
+ * moe_swiglu_backward, the program's products, moe_route_backward, moe_unsort without weights.
+ *
+ * In these five calls a row is a row of the sorted order that moe_dispatch makes: N rows (p->capacity = 0), or
+ * E * capacity rows of which expert e uses the first counts[e] of its own (at most capacity).  inv_perm[s] is the
+ * row of slot s; -1 says that the slot has none (a program that drops what an expert has no room for): it adds
+ * nothing, and nothing of it is read.  Any other number outside the rows does the same and is reported as
+ * MOE_ERR_BAD_ROUTING in status_dev (int32 on the device, may be NULL, written only on failure).  No two slots may
+ * have the same row.  `counts` is needed where rows are padded and may be NULL where they are not; unused rows are
+ * never read, and come out as zeros.  Sums are fp32; tensors of `dtype` and codes start on 16 bytes
+ * (else MOE_ERR_INVALID_ARG).  Outputs may not overlap inputs except where it says so.  The calls keep nothing
+ * and clear nothing: the same inputs give the same bits.
+ */
+
+/*
+ * Sorted rows back to their tokens: out[t] = addend[t] + sum_j topk_w[t,j] * rows[inv_perm[t*k+j]], one rounding.
+ *   topk_w NULL: weights one; that is the gradient of moe_dispatch's x_perm with respect to x (rows = dx_perm).
+ *   addend [T,d] dtype, may be NULL, may be `out`.
+ */
+int moe_unsort(const moe_problem_t *p, const void *rows, const int32_t *inv_perm, const float *topk_w,
+               const void *addend, void *out, int32_t *status_dev, void *stream);
+
+/*
+ * The gradient of moe_unsort: drows[inv_perm[t*k+j]] = topk_w[t,j] * dout[t], dtopk_w[t,j] = <rows[inv_perm[t*k+j]],
+ * dout[t]>, 0 for a slot without a row.
+ *   drows, dtopk_w: either may be NULL.  rows may be NULL if dtopk_w is; drows may be `rows`.  topk_w NULL: weights
+ *   one.  Rows that no slot names keep what drows held (ragged), unused rows become zero (padded).
+ */
+int moe_unsort_backward(const moe_problem_t *p, const void *dout, const void *rows, const int32_t *inv_perm,
+                        const float *topk_w, const int32_t *counts, void *drows, float *dtopk_w,
+                        int32_t *status_dev, void *stream);
+
+/* Host, pure: bytes of workspace moe_route_backward needs (any content); 0 if the problem is invalid. */
+size_t moe_backward_workspace_bytes(const moe_problem_t *p);
+
+/*
+ * The gradient of moe_route.  With topk_w the softmax over the k chosen logits and dl[t,j] = topk_w[t,j] *
+ * (dtopk_w[t,j] - sum_i topk_w[t,i] dtopk_w[t,i]): dx[t] = sum_j dl[t,j] Wg[:,topk_idx[t,j]], one rounding;
+ * dWg[:,e] and dgate_bias[e] = the sums of dl x[t] and of dl over the slots that chose e.
+ *   dx [T,d] dtype, dWg [d,E] fp32, dgate_bias [E] fp32 out; each may be NULL.  Wg is needed for dx, x for dWg.
+ *   An id outside [0,E) is MOE_ERR_BAD_ROUTING in status_dev; its slot has no gradient (its share of the sum over i
+ *   counts).  workspace: moe_backward_workspace_bytes() bytes, 256-byte aligned; needed for dWg and dgate_bias.
+ */
+int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx,
+                       const float *topk_w, const float *dtopk_w, void *dx, float *dWg, float *dgate_bias,
+                       int32_t *status_dev, void *workspace, void *stream);
+
+/*
+ * The experts' activation, h = silu(g) * u with silu(g) = g / (1 + exp(-g)), and its inputs kept for the backward
+ * pass in 8 bits.
+ *   g, u: [rows, f] dtype, `ld` elements from one row to the next in both (>= f, whole multiples of 16 bytes): two
+ *   tensors of their own, or the halves of one [rows, 2f].  h [rows, f] out, may be NULL.
+ *   codes [rows][2][f] bytes, scales [rows][2][ceil(f/32)] bytes out (g first, then u); both or none may be NULL.
+ *   Every 32 values of a row (the last 16, where f is an odd multiple of 16) share a power of two: scales holds its
+ *   exponent + 127 (E8M0), the least that brings the block's largest finite value to 448 or less, at least 0; codes
+ *   holds value / 2^exponent as e4m3 (OCP), rounded to nearest even.  A value that is not finite becomes the code of
+ *   a NaN; the others of its block are kept as without it.
+ */
+int moe_swiglu(const moe_problem_t *p, const void *g, const void *u, int64_t ld, const int32_t *counts, void *h,
+               uint8_t *codes, uint8_t *scales, void *stream);
+
+/*
+ * The gradient of moe_swiglu from what it kept: with g and u as decoded and s = 1 / (1 + exp(-g)),
+ * dg = dh u s (1 + g (1 - s)), du = dh g s, and h = g s u once more (for dW2 = h^T dy).
+ *   dh [rows, f] dtype in; dg, du [rows, f] dtype out with `ld` elements from one row to the next, as above; h
+ *   [rows, f] dtype out, may be NULL.
+ */
+int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *codes, const uint8_t *scales,
+                        const int32_t *counts, void *dg, void *du, int64_t ld, void *h, void *stream);
+
+/*
  * Measurement aid, no part of the layer: the rate at which this GPU's matrix cores retire bf16 work when nothing
  * else happens (what the grouped GEMM's "fraction of the MFMA peak" can be held against on a given box; the clock
  * a chip holds under matrix-core load depends on its power limit and on the operand bits).  `workgroups` workgroups

@@ -23,7 +23,8 @@ MOE_NUM_STATS = 20
 
 EXPORTS = ("moe_workspace_bytes", "moe_num_flags", "moe_status_string", "moe_workspace_init", "moe_route",
            "moe_dispatch", "moe_dispatch_noalloc", "moe_megakernel_forward", "moe_combine", "moe_probe_mfma",
-           "moe_probe_stream")
+           "moe_probe_stream", "moe_unsort", "moe_unsort_backward", "moe_backward_workspace_bytes", "moe_route_backward",
+           "moe_swiglu", "moe_swiglu_backward")
 
 
 class MoeProblem(ctypes.Structure):
@@ -61,8 +62,16 @@ _lib.moe_combine.argtypes = [_pp] + [_vp] * 7
 _lib.moe_probe_mfma.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, _vp, _vp]
 _lib.moe_probe_stream.argtypes = [_vp, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int32,
                                   ctypes.c_int32, _vp, _vp]
+_lib.moe_unsort.argtypes = [_pp] + [_vp] * 7
+_lib.moe_unsort_backward.argtypes = [_pp] + [_vp] * 9
+_lib.moe_backward_workspace_bytes.restype = ctypes.c_size_t
+_lib.moe_backward_workspace_bytes.argtypes = [_pp]
+_lib.moe_route_backward.argtypes = [_pp] + [_vp] * 11
+_lib.moe_swiglu.argtypes = [_pp, _vp, _vp, ctypes.c_int64] + [_vp] * 5
+_lib.moe_swiglu_backward.argtypes = [_pp] + [_vp] * 6 + [ctypes.c_int64, _vp, _vp]
 for _n in ("moe_workspace_init", "moe_route", "moe_dispatch", "moe_dispatch_noalloc", "moe_megakernel_forward",
-           "moe_combine", "moe_probe_mfma", "moe_probe_stream"):
+           "moe_combine", "moe_probe_mfma", "moe_probe_stream", "moe_unsort", "moe_unsort_backward", "moe_route_backward",
+           "moe_swiglu", "moe_swiglu_backward"):
     getattr(_lib, _n).restype = ctypes.c_int
 
 
@@ -139,6 +148,45 @@ def moe_megakernel_forward(p, x, Wg, gate_bias, W1, W3, W2, topk_idx, topk_w, co
 def moe_combine(p, staging, flags, slot_flag, topk_w, out, status_dev, stream=None):
     _check(_lib.moe_combine(ctypes.byref(p), _ptr(staging), _ptr(flags), _ptr(slot_flag), _ptr(topk_w), _ptr(out),
                             _ptr(status_dev), _stream(stream)), "moe_combine")
+
+
+def moe_unsort(p, rows, inv_perm, topk_w, addend, out, status_dev, stream=None):
+    _check(_lib.moe_unsort(ctypes.byref(p), _ptr(rows), _ptr(inv_perm), _ptr(topk_w), _ptr(addend), _ptr(out),
+                           _ptr(status_dev), _stream(stream)), "moe_unsort")
+
+
+def moe_unsort_backward(p, dout, rows, inv_perm, topk_w, counts, drows, dtopk_w, status_dev, stream=None):
+    _check(_lib.moe_unsort_backward(ctypes.byref(p), _ptr(dout), _ptr(rows), _ptr(inv_perm), _ptr(topk_w), _ptr(counts),
+                                    _ptr(drows), _ptr(dtopk_w), _ptr(status_dev), _stream(stream)), "moe_unsort_backward")
+
+
+def moe_backward_workspace_bytes(p: MoeProblem) -> int:
+    return int(_lib.moe_backward_workspace_bytes(ctypes.byref(p)))
+
+
+def moe_route_backward(p, x, Wg, topk_idx, topk_w, dtopk_w, dx, dWg, dgate_bias, status_dev, workspace, stream=None):
+    _check(_lib.moe_route_backward(ctypes.byref(p), _ptr(x), _ptr(Wg), _ptr(topk_idx), _ptr(topk_w), _ptr(dtopk_w), _ptr(dx),
+                                   _ptr(dWg), _ptr(dgate_bias), _ptr(status_dev), _ptr(workspace), _stream(stream)),
+           "moe_route_backward")
+
+
+def _row_ptrs(a, b):
+    """Two [rows, f] tensors or views whose rows are the same number of elements apart: both addresses, and that number."""
+    assert a.is_cuda and b.is_cuda and a.stride(1) == b.stride(1) == 1 and a.shape == b.shape, "device tensors, rows of one piece"
+    assert a.shape[0] == 1 or a.stride(0) == b.stride(0), "rows the same number of elements apart"
+    return ctypes.c_void_p(a.data_ptr()), ctypes.c_void_p(b.data_ptr()), a.stride(0) if a.shape[0] > 1 else a.shape[1]
+
+
+def moe_swiglu(p, g, u, counts, h, codes, scales, stream=None):
+    gp, up, ld = _row_ptrs(g, u)
+    _check(_lib.moe_swiglu(ctypes.byref(p), gp, up, ld, _ptr(counts), _ptr(h), _ptr(codes), _ptr(scales), _stream(stream)),
+           "moe_swiglu")
+
+
+def moe_swiglu_backward(p, dh, codes, scales, counts, dg, du, h, stream=None):
+    gp, up, ld = _row_ptrs(dg, du)
+    _check(_lib.moe_swiglu_backward(ctypes.byref(p), _ptr(dh), _ptr(codes), _ptr(scales), _ptr(counts), gp, up, ld, _ptr(h),
+                                    _stream(stream)), "moe_swiglu_backward")
 
 
 def moe_probe_mfma(frag, iters, workgroups, sink, stream=None):

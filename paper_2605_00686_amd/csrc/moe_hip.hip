@@ -691,6 +691,11 @@ static int make_plan(const moe_problem_t *p, Plan *pl) {
     return MOE_OK;
 }
 
+int check_problem(const moe_problem_t *p) {
+    Plan pl;
+    return make_plan(p, &pl);
+}
+
 static void fill_args(const Plan &pl, void *workspace, KArgs *a) {
     const moe_problem_t &p = pl.p;
     memset(a, 0, sizeof(*a));

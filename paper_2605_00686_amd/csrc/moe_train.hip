@@ -1,0 +1,148 @@
+// C ABI of the calls that train the layer around a program's own expert products: argument checks and launches.  Declarations and
+// contracts live in include/moe.h.
+#include <hip/hip_runtime.h>
+
+#include "gate_grad.hpp"
+#include "problem.hpp"
+#include "swiglu8.hpp"
+#include "unsort.hpp"
+
+using namespace moe;
+
+static int launched() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+static int rows_of(const moe_problem_t *p) { return p->capacity > 0 ? p->E * p->capacity : p->T * p->k; }
+static int elem_bytes(const moe_problem_t *p) { return p->dtype == MOE_DT_F32 ? 4 : 2; }
+// Workgroups for `n` pieces of work, `each` of them per workgroup; the kernels take more in strides of the grid.
+static unsigned grid_for(size_t n, size_t each) {
+    const size_t g = (n + each - 1) / each;
+    return (unsigned)(g < (1u << 20) ? g : (1u << 20));
+}
+
+extern "C" {
+
+int moe_unsort(const moe_problem_t *p, const void *rows, const int32_t *inv_perm, const float *topk_w, const void *addend, void *out,
+               int32_t *status_dev, void *stream) {
+    const int rc = check_problem(p);
+    if (rc) return rc;
+    if (!rows || !inv_perm || !out) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(rows) || !aligned16(addend) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
+    UnsortArgs a = {};
+    a.T = p->T; a.d = p->d; a.k = p->k; a.rows = rows_of(p);
+    a.sorted = rows; a.inv_perm = inv_perm; a.w = topk_w; a.addend = addend; a.out = out; a.status = status_dev;
+    const dim3 grid(grid_for(p->T, 4));
+    hipStream_t st = (hipStream_t)stream;
+    if (p->dtype == MOE_DT_F32)
+        hipLaunchKernelGGL(k_unsort<float>, grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(k_unsort<bf16_t>, grid, dim3(kThreads), 0, st, a);
+    return launched();
+}
+
+int moe_unsort_backward(const moe_problem_t *p, const void *dout, const void *rows, const int32_t *inv_perm, const float *topk_w,
+                        const int32_t *counts, void *drows, float *dtopk_w, int32_t *status_dev, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!dout || !inv_perm || (!drows && !dtopk_w) || (dtopk_w && !rows)) return MOE_ERR_INVALID_ARG;
+    if (p->capacity > 0 && !counts) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(dout) || !aligned16(rows) || !aligned16(drows)) return MOE_ERR_INVALID_ARG;
+    UnsortArgs a = {};
+    a.T = p->T; a.d = p->d; a.k = p->k; a.rows = rows_of(p); a.capacity = p->capacity; a.E = p->E;
+    a.dout = dout; a.sorted = rows; a.inv_perm = inv_perm; a.w = topk_w; a.counts = counts; a.drows = drows; a.dw = dtopk_w;
+    a.status = status_dev;
+    hipStream_t st = (hipStream_t)stream;
+    const dim3 grid(grid_for(p->T, 4));
+    if (p->dtype == MOE_DT_F32)
+        hipLaunchKernelGGL(k_unsort_backward<float>, grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(k_unsort_backward<bf16_t>, grid, dim3(kThreads), 0, st, a);
+    if ((rc = launched())) return rc;
+    if (p->capacity > 0 && drows) {
+        hipLaunchKernelGGL(k_zero_unused, dim3(grid_for(a.rows, 4)), dim3(kThreads), 0, st, counts, a.rows, p->capacity,
+                           (size_t)p->d * elem_bytes(p), drows);
+        rc = launched();
+    }
+    return rc;
+}
+
+size_t moe_backward_workspace_bytes(const moe_problem_t *p) { return check_problem(p) == MOE_OK ? 256 : 0; }
+
+int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx, const float *topk_w,
+                       const float *dtopk_w, void *dx, float *dWg, float *dgate_bias, int32_t *status_dev, void *workspace, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!topk_idx || !topk_w || !dtopk_w || (!dx && !dWg && !dgate_bias)) return MOE_ERR_INVALID_ARG;
+    if ((dx && !Wg) || (dWg && !x)) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(Wg) || !aligned16(dx) || !aligned16(dWg)) return MOE_ERR_INVALID_ARG;
+    if ((dWg || dgate_bias) && (!workspace || ((uintptr_t)workspace & 255) != 0)) return MOE_ERR_WORKSPACE;
+    GateGradArgs a = {};
+    a.T = p->T; a.d = p->d; a.E = p->E; a.k = p->k;
+    a.x = dWg ? x : nullptr; a.Wg = Wg; a.idx = topk_idx; a.w = topk_w; a.dw = dtopk_w; a.dx = dx; a.dWg = dWg; a.dbias = dgate_bias;
+    a.status = status_dev;
+    hipStream_t st = (hipStream_t)stream;
+    if (dx) {
+        const dim3 grid(grid_for((size_t)p->T * p->d * elem_bytes(p) / 16, kThreads));
+        if (p->dtype == MOE_DT_F32)
+            hipLaunchKernelGGL(k_gate_dx<float>, grid, dim3(kThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL(k_gate_dx<bf16_t>, grid, dim3(kThreads), 0, st, a);
+        if ((rc = launched())) return rc;
+    }
+    if (dWg || dgate_bias) {
+        const dim3 grid(p->E, dWg ? (p->d + kThreads - 1) / kThreads : 1);
+        if (p->dtype == MOE_DT_F32)
+            hipLaunchKernelGGL(k_gate_dw<float>, grid, dim3(kThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL(k_gate_dw<bf16_t>, grid, dim3(kThreads), 0, st, a);
+        rc = launched();
+    }
+    return rc;
+}
+
+static int check_swiglu(const moe_problem_t *p, int64_t ld, const int32_t *counts, const void *codes, const void *scales) {
+    if (p->capacity > 0 && !counts) return MOE_ERR_INVALID_ARG;
+    if (ld < p->f || ld * elem_bytes(p) % 16 != 0) return MOE_ERR_INVALID_ARG;
+    if (!codes != !scales || !aligned16(codes)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+int moe_swiglu(const moe_problem_t *p, const void *g, const void *u, int64_t ld, const int32_t *counts, void *h, uint8_t *codes,
+               uint8_t *scales, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!g || !u || (!h && !codes)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_swiglu(p, ld, counts, codes, scales))) return rc;
+    if (!aligned16(g) || !aligned16(u) || !aligned16(h)) return MOE_ERR_INVALID_ARG;
+    SwigluArgs a = {};
+    a.rows = rows_of(p); a.f = p->f; a.capacity = p->capacity; a.ld = ld;
+    a.g = g; a.u = u; a.counts = counts; a.h = h; a.codes = codes; a.scales = scales;
+    const dim3 grid(grid_for((size_t)a.rows * ((p->f + kScaleBlock - 1) / kScaleBlock * 4), kThreads));
+    hipStream_t st = (hipStream_t)stream;
+    if (p->dtype == MOE_DT_F32)
+        hipLaunchKernelGGL(k_swiglu<float>, grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(k_swiglu<bf16_t>, grid, dim3(kThreads), 0, st, a);
+    return launched();
+}
+
+int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *codes, const uint8_t *scales, const int32_t *counts,
+                        void *dg, void *du, int64_t ld, void *h, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!dh || !codes || !dg || !du) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_swiglu(p, ld, counts, codes, scales))) return rc;
+    if (!aligned16(dh) || !aligned16(dg) || !aligned16(du) || !aligned16(h)) return MOE_ERR_INVALID_ARG;
+    SwigluArgs a = {};
+    a.rows = rows_of(p); a.f = p->f; a.capacity = p->capacity; a.ld = ld;
+    a.dh = dh; a.counts = counts; a.dg = dg; a.du = du; a.h = h;
+    a.codes = const_cast<uint8_t *>(codes); a.scales = const_cast<uint8_t *>(scales);
+    const dim3 grid(grid_for((size_t)a.rows * (p->f / kLaneValues), kThreads));
+    hipStream_t st = (hipStream_t)stream;
+    if (p->dtype == MOE_DT_F32)
+        hipLaunchKernelGGL(k_swiglu_backward<float>, grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(k_swiglu_backward<bf16_t>, grid, dim3(kThreads), 0, st, a);
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,49 @@
+// Rows in pieces of 16 bytes, as the training calls move them.  gfx950 only.
+#pragma once
+#include "common.hpp"
+
+namespace moe {
+
+template <typename ET> struct Piece;
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void unpack(const u32x4_t &v, float *f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+    }
+    static __device__ __forceinline__ u32x4_t pack(const float *f) {
+        return u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+};
+template <> struct Piece<bf16_t> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void unpack(const u32x4_t &v, float *f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(v[i] << 16);
+            f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4_t pack(const float *f) {
+        return u32x4_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+    }
+};
+
+// A lane's value from the lane whose number differs in bit 0 (0xB1) or bit 1 (0x4E): no trip through LDS.
+template <int QUAD>
+__device__ __forceinline__ u32 quad_swap(u32 v) {
+    return (u32)__builtin_amdgcn_update_dpp(0, (int)v, QUAD, 0xf, 0xf, true);
+}
+
+__device__ __forceinline__ void report(int32_t *status, int code) {
+    if (status) *status = code;  // (whoever writes, writes the same)
+}
+
+// The row of a slot, or -1: none, or none that exists, which is reported.
+__device__ __forceinline__ int row_of_slot(int row, int rows, int32_t *status) {
+    if ((u32)row < (u32)rows) return row;
+    if (row != -1) report(status, MOE_ERR_BAD_ROUTING);
+    return -1;
+}
+
+}  // namespace moe
