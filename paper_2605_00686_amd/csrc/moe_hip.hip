@@ -10,6 +10,7 @@
 #include "common.hpp"
 #include "dispatch.hpp"
 #include "expert.hpp"
+#include "problem.hpp"
 #include "route.hpp"
 
 namespace moe {
@@ -811,6 +812,7 @@ static int set_smem_raw(const void *kernel, size_t bytes) {
         table[n++] = Entry{dev, kernel, bytes};
     return MOE_OK;
 }
+int allow_lds(const void *kernel, size_t bytes) { return set_smem_raw(kernel, bytes); }
 template <class K>
 static int set_smem(K kernel, size_t bytes) {
     return set_smem_raw((const void *)kernel, bytes);
