@@ -1,86 +1,110 @@
 // The gradient of the gate: softmax over the chosen logits, x Wg.
 //
-// With dl[t,j] = w[t,j] (dw[t,j] - sum_i w[t,i] dw[t,i]), token t has k numbers that are not zero among E: both products,
-// dx = dl Wg^T and dWg = x^T dl, are taken over those alone, so that what no token chose has no part in it (a dense product would turn a
-// zero times an infinity into a NaN of every expert), on the vector ALU in fp32.  A task works on the columns of a chunk: 256
-// bytes of a row, 16 lanes with 16 bytes each, four tokens' (or slots') rows per instruction of a wavefront.
+// With dl[t,j] = w[t,j] (dw[t,j] - sum_i w[t,i] dw[t,i]), token t has k numbers that are not zero among E.
+//
+// dx = dl Wg^T is taken over those alone, on the vector ALU: a task keeps a chunk's columns of Wg in LDS, by expert (256 bytes of
+// every column), and 16 lanes add up a token's k pieces.
+//
+// dWg = x^T dl is a product of the matrix cores, with the zeros: one instruction takes 16 tokens x 32 columns x 32 experts, and the
+// dense product costs less than listing the slots by expert does (see gate_dw_task).  fp32 numbers are cut into three bf16
+// numbers that add up to them exactly (8 bits each, truncated), so the products lose nothing; a number of x that is not
+// finite is left out of the dense product, where it would make a NaN of every expert's sum, and added for its token's experts alone.
 #pragma once
+#include <type_traits>
+
 #include "pieces.hpp"
 
 namespace moe {
 
-constexpr int kGateGradThreads = 1024, kGateGradWaves = kGateGradThreads / 64;
-constexpr int kChunkBytes = 256;       // of a row of x, of dx, and of a column of Wg
-constexpr int kGateGradSlots = 2048;   // slots of a block of tokens, at most
-constexpr int kGateGradTokens = 256;   // tokens of a block, at most
+constexpr int kGateGradThreads = 512, kGateGradWaves = kGateGradThreads / 64;
+constexpr int kChunkBytes = 256;      // dx: of a row, and of a column of Wg
+constexpr int kGateDwCols = 64;       // dWg: columns of a task
+constexpr int kGateGradSlots = 1024;  // dx: slots of a block of tokens, at most
 
 struct GateGradArgs {
     int T, d, E, k;
-    int block;         // tokens of a block: block * k <= kGateGradSlots
-    int chunks, dw_chunks;     // of columns; those that dWg's tasks take (one if dbias alone is wanted)
-    int dw_parts;      // the tokens of dWg's sums are cut into so many parts, whole blocks each (0: no dWg and no dbias wanted)
-    int dx_parts;      // tokens per dx task, likewise (0: no dx wanted)
-    int dw_blocks, dx_blocks;  // blocks of a part
+    int dx_chunks;             // dx: chunks of columns
+    int block;                 // dx: tokens of a block: block * k <= kGateGradSlots
+    int dx_parts, dx_blocks;   // dx: the tokens are cut into so many parts (0: no dx wanted) of so many blocks
+    int dw_chunks;             // dWg: its chunks (0: not wanted)
+    int dw_parts, dw_tokens;   // dWg and dbias: the tokens are cut into so many parts (0: neither wanted) of so many (a multiple of a reduction block)
     const void *x, *Wg;
     const int32_t *idx;
     const float *w, *dw;
     void *dx;
-    float *dWg, *dbias;  // of one part (dw_parts == 1), else the parts' sums in the workspace, part_stride apart
+    float *dWg, *dbias;
+    float *parts;              // workspace: the parts' sums, dWg's [d][E] and dbias's [E], part_stride floats apart, if there is more than one part
     size_t part_stride;
     int32_t *status;
 };
 
 struct GateGradSlot {
-    int row;  // dx: the slot's expert, -1 = none; dWg: its token in the block
+    int row;  // the slot's expert, E = none
     float dl;
 };
 
-// LDS of a task, in this order (the transposition of a task's end takes the same bytes again)
-struct alignas(16) GateGradLds {
-    GateGradSlot slot[kGateGradSlots];
-    float prod[kGateGradSlots];
-    u64 chosen[kMaxExperts][kGateGradTokens / 64];  // dWg: the block's tokens that chose an expert, one bit each
-    int first[kMaxExperts + 1];                     // ... and the first of its slots
-    int wave_sum[4];
-    // behind it: a block's rows of x, or the chunk's columns of Wg by expert
-};
-
-// dl of the block's slots: calls `put(i, slot, expert or -1, dl)` for the slots that this thread has, its i-th.
-template <typename F>
-__device__ __forceinline__ void gate_block_slots(const GateGradArgs &a, GateGradLds *l, int t0, int n, F &&put) {
-    constexpr int PER = kGateGradSlots / kGateGradThreads;
+// Slots of tokens in registers: G lanes (the power of two from 8 on that holds k) take a token, kGateGradThreads / G tokens a pass.
+__device__ __forceinline__ int gate_lanes_log2(int k) { return k <= 8 ? 3 : k <= 16 ? 4 : 5; }
+// A sum over the 8, 16 or 32 lanes of a token, in every one of them.
+__device__ __forceinline__ float gate_lanes_sum(float v, int log2) {
+    auto add = [&](auto ctrl) { v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    add(std::integral_constant<int, 0xB1>());   // the neighbour,
+    add(std::integral_constant<int, 0x4E>());   // the other pair of four,
+    add(std::integral_constant<int, 0x141>());  // the other four of eight (mirrored; within four all have the same),
+    if (log2 > 3) add(std::integral_constant<int, 0x140>());  // the other eight of sixteen
+    if (log2 > 4) v += __shfl_xor(v, 16);
+    return v;
+}
+template <int PER>
+struct GateSlots {
     float w[PER], dw[PER];
     int e[PER];
-    const int slots = n * a.k;
+    // (whether the i-th pass lies past n tokens)
+    static __device__ __forceinline__ bool skip(int i, int log2, int n) { return i > 0 && ((i * kGateGradThreads) >> log2) >= n; }
+    // tokens t0 .. t0 + n - 1
+    __device__ __forceinline__ void load(const GateGradArgs &a, int log2, int t0, int n) {
+        const int j = threadIdx.x & ((1 << log2) - 1);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = threadIdx.x + i * kGateGradThreads;
-        if (s >= slots) continue;
-        const size_t g = (size_t)t0 * a.k + s;
-        w[i] = a.w[g], dw[i] = a.dw[g], e[i] = a.idx[g];
-        l->prod[s] = w[i] * dw[i];
+        for (int i = 0; i < PER; ++i) {
+            if (skip(i, log2, n)) continue;
+            const int t = (threadIdx.x + i * kGateGradThreads) >> log2;
+            const bool in = t < n && j < a.k;
+            const u32 s = in ? (u32)(t0 + t) * (u32)a.k + j : 0u;  // (T k is at most 2^30)
+            w[i] = a.w[s], dw[i] = a.dw[s], e[i] = a.idx[s];
+            if (!in) w[i] = dw[i] = 0.f;
+        }
     }
-    __syncthreads();
+    // put(i, token, choice, expert or -1, dl) for those of the tokens' slots that this thread has, its i-th
+    template <typename F>
+    __device__ __forceinline__ void finish(const GateGradArgs &a, int log2, int n, F &&put) {
+        const int j = threadIdx.x & ((1 << log2) - 1);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = threadIdx.x + i * kGateGradThreads;
-        if (s >= slots) continue;
-        const int from = s / a.k * a.k;
-        float mean = 0.f;
-        for (int j = 0; j < a.k; ++j) mean += l->prod[from + j];
-        if ((u32)e[i] >= (u32)a.E) report(a.status, MOE_ERR_BAD_ROUTING), e[i] = -1;
-        put(i, s, e[i], w[i] * (dw[i] - mean));
+        for (int i = 0; i < PER; ++i) {
+            if (skip(i, log2, n)) continue;
+            const int t = (threadIdx.x + i * kGateGradThreads) >> log2;
+            const float dl = w[i] * (dw[i] - gate_lanes_sum(w[i] * dw[i], log2));
+            if (t >= n || j >= a.k) continue;
+            if ((u32)e[i] >= (u32)a.E) report(a.status, MOE_ERR_BAD_ROUTING), e[i] = -1;
+            put(i, t, j, e[i], dl);
+        }
     }
-}
+};
+
+// LDS of a dx task; behind it the chunk's columns of Wg by expert, and one of zeros
+struct alignas(16) GateDxLds {
+    GateGradSlot slot[kGateGradSlots];
+};
 
 // dx[tokens of a part, columns of a chunk] = sum_j dl Wg[:, e_j]
 template <typename ET>
 __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, int chunk, int part) {
     using P = Piece<ET>;
     constexpr int COLS = kChunkBytes / (int)sizeof(ET);
-    GateGradLds *l = (GateGradLds *)smem;
-    char *wt = smem + sizeof(GateGradLds);  // [E][COLS]
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col0 = chunk * COLS;
+    GateDxLds *l = (GateDxLds *)smem;
+    char *wt = smem + sizeof(GateDxLds);  // [E + 1][COLS]
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col0 = chunk * COLS, log2 = gate_lanes_log2(a.k);
+    GateSlots<kGateGradSlots / kGateGradThreads> slots;
+    slots.load(a, log2, part * a.dx_blocks * a.block, min(a.block, a.T - part * a.dx_blocks * a.block));
     // the chunk's rows of Wg, by expert: a wavefront takes some experts of all rows, so that its lanes write side by side
     if constexpr (sizeof(ET) == 2) {
         const int i = min(col0 + 2 * lane, a.d - 2);
@@ -102,182 +126,284 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
         const float *row = (const float *)a.Wg + (size_t)min(col0 + lane, a.d - 1) * a.E;
         for (int e = wave; e < a.E; e += kGateGradWaves) *(float *)(wt + e * kChunkBytes + lane * 4) = row[e];
     }
+    if (wave == 0) *(u32 *)(wt + a.E * kChunkBytes + lane * 4) = 0u;
     const int group = threadIdx.x / 16, l16 = lane & 15, col = col0 + l16 * P::N;
     for (int b = 0; b < a.dx_blocks; ++b) {
         const int t0 = (part * a.dx_blocks + b) * a.block, n = min(a.block, a.T - t0);
         if (n <= 0) break;
         __syncthreads();
-        gate_block_slots(a, l, t0, n, [&](int, int s, int e, float dl) { l->slot[s] = GateGradSlot{e, dl}; });
+        slots.finish(a, log2, n, [&](int, int t, int j, int e, float dl) { l->slot[t * a.k + j] = e < 0 ? GateGradSlot{a.E, 0.f} : GateGradSlot{e, dl}; });
         __syncthreads();
+        slots.load(a, log2, t0 + a.block, b + 1 < a.dx_blocks ? min(a.block, a.T - t0 - a.block) : 0);
         for (int t = group; t < n; t += kGateGradThreads / 16) {
             float acc[P::N] = {};
-            for (int j = 0; j < a.k; ++j) {
-                const GateGradSlot s = l->slot[t * a.k + j];
-                if (s.row < 0) continue;
-                float f[P::N];
-                P::unpack(*(const u32x4_t *)(wt + s.row * kChunkBytes + l16 * 16), f);
+            const GateGradSlot *mine = l->slot + t * a.k;
+            // (four rows at a time, the last ones made up with rows of zeros)
+            for (int j = 0; j < a.k; j += 4) {
+                GateGradSlot s[4];
+                u32x4_t v[4];
 #pragma unroll
-                for (int i = 0; i < P::N; ++i) acc[i] = fmaf(s.dl, f[i], acc[i]);
+                for (int i = 0; i < 4; ++i) {
+                    s[i] = mine[min(j + i, a.k - 1)];
+                    if (j + i >= a.k) s[i] = GateGradSlot{a.E, 0.f};
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = *(const u32x4_t *)(wt + s[i].row * kChunkBytes + l16 * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float f[P::N];
+                    P::unpack(v[i], f);
+#pragma unroll
+                    for (int q = 0; q < P::N; ++q) acc[q] = fmaf(s[i].dl, f[q], acc[q]);
+                }
             }
             if (col < a.d) *(u32x4_t *)((ET *)a.dx + (size_t)(t0 + t) * a.d + col) = P::pack(acc);
         }
     }
 }
 
-// A sum over the four groups of 16 lanes, dealt out: of N values per lane, a lane keeps N / 4.  Value i of group 0 .. 3 is then value
-// i + N/2 * (upper 32 lanes) + N/4 * (upper 16 of 32).
-template <int N>
-__device__ __forceinline__ void sum_groups(float *v) {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
-        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 4]), false, false);
-        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
+// A finite fp32 number as three bf16 numbers (their bits), 8 bits of it each; one that is not: itself and zeros.
+__device__ __forceinline__ void cut3(float v, u32 *b) {
+    const u32 h = __float_as_uint(v) & 0xffff0000u;
+    const float r = v - __uint_as_float(h);
+    const u32 m = __float_as_uint(r) & 0xffff0000u;
+    const float s = r - __uint_as_float(m);
+    const bool finite = (h & 0x7f800000u) != 0x7f800000u;
+    // (a NaN keeps a bit that survives the cut)
+    b[0] = finite ? h >> 16 : (__float_as_uint(v) >> 16) | ((__float_as_uint(v) & 0x7fffffu) ? 0x40u : 0u);
+    b[1] = finite ? m >> 16 : 0u;
+    b[2] = finite ? __float_as_uint(s) >> 16 : 0u;
 }
 
-// dWg[columns of a chunk, :] and dbias over the tokens of a part.  A block's slots are listed by expert (their places counted from bit
-// masks, so the order of every sum is that of the tokens); a wavefront takes every 16th expert and keeps its sums in registers from
-// block to block.  NE = experts per wavefront, at most.
-template <typename ET, int NE>
+// Shape of a dWg task: 8 wavefronts as 4 x 2, each with EB blocks of 32 experts x 32 columns; KT tokens per reduction block.
+template <typename ET_, int EB_, int KT_>
+struct GateDwShape {
+    using ET = ET_;
+    static constexpr int EB = EB_, KT = KT_, WE = 4, COLS = kGateDwCols, EPAD = EB * WE * 32;
+    static constexpr int XP = sizeof(ET) == 4 ? 3 : 1;  // bf16 numbers that make up one of x
+    // Rows of LDS.  dl, [3][EPAD][KT] bf16: 16 bytes behind each row, so that 16 lanes' pieces of 16 bytes meet no bank twice; x,
+    // [XP][KT][COLS] bf16: rows 16 banks apart modulo 64, for the transposing read of 4 rows x 64 bytes.
+    static constexpr int DROW = KT * 2 + 16, XROW = COLS * 2 + 64;
+    static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
+    static constexpr int O_X = 3 * DPLANE, O_ODD = O_X + XP * XPLANE, LDS = O_ODD + 16;
+    static constexpr int PER = KT * 32 / kGateGradThreads;        // slots of a reduction block per thread, at most
+    static constexpr int LANES = COLS / Piece<ET>::N;             // of a row of x, a piece each
+    static_assert(KT * LANES <= kGateGradThreads, "a piece per thread");
+};
+using GateDw16M = GateDwShape<bf16_t, 1, 64>;  // up to 128 experts
+using GateDw16L = GateDwShape<bf16_t, 2, 32>;  // 256
+using GateDw32M = GateDwShape<float, 1, 32>;
+using GateDw32L = GateDwShape<float, 2, 32>;
+
+// dWg[columns of a chunk, :] over the tokens of a part.  For a reduction block of tokens dl
+// lies dense in LDS, by expert: its slots are written there, multiplied, and cleared again.
+template <class C>
 __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, int chunk, int part) {
+    using ET = typename C::ET;
     using P = Piece<ET>;
-    constexpr int COLS = kChunkBytes / (int)sizeof(ET), KEEP = P::N / 4;
-    GateGradLds *l = (GateGradLds *)smem;
-    char *tile = smem + sizeof(GateGradLds);  // [tokens][COLS]
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = chunk * COLS;
-    const int l16 = lane & 15, group = lane >> 4, words = (a.block + 63) / 64;
-    float acc[NE][KEEP], bias = 0.f;  // (lane n keeps that of the wavefront's n-th expert)
+    typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+    typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int col0 = chunk * C::COLS, log2 = gate_lanes_log2(a.k);
+    const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
+    char *xs = smem + C::O_X;
+    int *odd = (int *)(smem + C::O_ODD);  // first and last token whose x has a number here that is not finite
+    // Loads run four blocks ahead (x) and two (slots): a block's tokens are few, and a CU may have one workgroup
+    constexpr int XD = 4, SD = 2;
+    u32x4_t rows[XD];
+    GateSlots<C::PER> slots[SD];
+    const int x_tok = tid / C::LANES, x_lane = tid % C::LANES;
+    const ET *x = (const ET *)a.x + min(col0 + x_lane * P::N, a.d - P::N);
+    auto load_x = [&](u32x4_t &v, int t0) {
+        if (t0 < t_end && x_tok < C::KT) v = *(const u32x4_t *)(x + (size_t)min(t0 + x_tok, t_end - 1) * a.d);
+    };
 #pragma unroll
-    for (int n = 0; n < NE; ++n)
+    for (int i = 0; i < SD; ++i) slots[i].load(a, log2, t_begin + i * C::KT, min(C::KT, t_end - t_begin - i * C::KT));
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) acc[n][i] = 0.f;
-    for (int b = 0; b < a.dw_blocks; ++b) {
-        const int t0 = (part * a.dw_blocks + b) * a.block, n_tok = min(a.block, a.T - t0);
-        if (n_tok <= 0) break;
-        u32x4_t rows[4];
-        if (a.x) {
+    for (int i = 0; i < XD; ++i) load_x(rows[i], t_begin + i * C::KT);
+    for (int i = tid * 16; i < C::O_X; i += kGateGradThreads * 16) *(u32x4_t *)(smem + i) = u32x4_t{0, 0, 0, 0};
+    if (tid == 0) odd[0] = 0x7fffffff, odd[1] = -1;
+    const int we = wave % C::WE, wc = wave / C::WE, e0 = we * C::EB * 32, c0 = wc * 32;
+    f32x16_t acc[C::EB];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = min(tid / 16 + i * (kGateGradThreads / 16), n_tok - 1), c = min(col0 + l16 * P::N, a.d - P::N);
-                rows[i] = *(const u32x4_t *)((const ET *)a.x + (size_t)(t0 + t) * a.d + c);
+    for (int i = 0; i < C::EB; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][q] = 0.f;
+    auto put_x = [&](u32x4_t v, int t0) {
+        if (x_tok >= C::KT) return;
+        const bool in = t0 + x_tok < t_end;
+        bool strange = false;
+        if constexpr (sizeof(ET) == 2) {
+            u32 carry = 0u;  // of exponents that are all ones
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v[q] = in ? v[q] : 0u;
+                carry |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
             }
+            strange = carry != 0u;
+            if (strange) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
+                    if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
+                }
+            }
+            *(u32x4_t *)(xs + x_tok * C::XROW + x_lane * 16) = v;
+        } else {
+            u32 b[4][3];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool fine = (v[q] & 0x7f800000u) != 0x7f800000u;
+                strange |= !fine;
+                cut3(in && fine ? __uint_as_float(v[q]) : 0.f, b[q]);
+            }
+#pragma unroll
+            for (int n = 0; n < 3; ++n)
+                *(uint2 *)(xs + n * C::XPLANE + x_tok * C::XROW + x_lane * 8) = uint2{b[0][n] | (b[1][n] << 16), b[2][n] | (b[3][n] << 16)};
         }
+        if (strange && in) atomicMin(&odd[0], t0 + x_tok), atomicMax(&odd[1], t0 + x_tok);
+    };
+    int at[C::PER];  // where this thread's slots lie in dl, -1 = it has none
+#pragma unroll
+    for (int i = 0; i < C::PER; ++i) at[i] = -1;
+    auto block = [&](int t0, u32x4_t &row, GateSlots<C::PER> &slot) {
         __syncthreads();  // (the block before is done with the LDS)
-        for (int i = tid; i < a.E * words; i += kGateGradThreads) l->chosen[i / words][i % words] = 0ull;
-        int es[2] = {-1, -1}, ts[2];
-        float dls[2];
-        gate_block_slots(a, l, t0, n_tok, [&](int i, int s, int e, float dl) {
-            es[i] = e, ts[i] = s / a.k, dls[i] = dl;
-            if (e >= 0) atomicOr(&l->chosen[e][ts[i] / 64], 1ull << (ts[i] & 63));
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i)
+            if (!GateSlots<C::PER>::skip(i, log2, C::KT) && at[i] >= 0) {
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = 0;
+                at[i] = -1;
+            }
+        put_x(row, t0);
+        load_x(row, t0 + XD * C::KT);
+        u32 cut[C::PER][3];
+        slot.finish(a, log2, min(C::KT, t_end - t0), [&](int i, int t, int, int e, float dl) {
+            at[i] = e < 0 ? -1 : e * C::DROW + t * 2;
+            cut3(dl, cut[i]);
         });
-        if (a.x) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (const int t = tid / 16 + i * (kGateGradThreads / 16); t < a.block) *(u32x4_t *)(tile + t * kChunkBytes + l16 * 16) = rows[i];
-        }
-        __syncthreads();
-        int count = 0, sum = 0;
-        if (tid < kMaxExperts) {
-            if (tid < a.E)
-                for (int i = 0; i < words; ++i) count += __popcll(l->chosen[tid][i]);
-            sum = count;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const int v = __shfl_up(sum, m);
-                if (lane >= m) sum += v;
-            }
-            if (lane == 63) l->wave_sum[wave] = sum;
-        }
-        __syncthreads();
-        if (tid < kMaxExperts) {
-            for (int i = 0; i < wave; ++i) sum += l->wave_sum[i];
-            if (tid < a.E) l->first[tid + 1] = sum;
-            if (tid == 0) l->first[0] = 0;
-        }
+        slot.load(a, log2, t0 + SD * C::KT, min(C::KT, t_end - t0 - SD * C::KT));
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (es[i] >= 0) {
-                const int t = ts[i];
-                int at = l->first[es[i]] + __popcll(l->chosen[es[i]][t / 64] & ((1ull << (t & 63)) - 1ull));
-                for (int m = 0; m < t / 64; ++m) at += __popcll(l->chosen[es[i]][m]);
-                l->slot[at] = GateGradSlot{t, dls[i]};
+        for (int i = 0; i < C::PER; ++i)
+            if (!GateSlots<C::PER>::skip(i, log2, C::KT) && at[i] >= 0) {
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)cut[i][n];
             }
         __syncthreads();
+        if (e0 >= a.E) return;
 #pragma unroll
-        for (int n = 0; n < NE; ++n) {
-            const int e = wave + n * kGateGradWaves;
-            if (e >= a.E) break;
-            const int from = uniform(l->first[e]), cnt = uniform(l->first[e + 1]) - from;
-            float v[P::N] = {}, vb = 0.f;
-            for (int i = group; i < cnt; i += 4) {
-                const GateGradSlot s = l->slot[from + i];
-                vb += s.dl;
-                if (a.x) {
-                    float f[P::N];
-                    P::unpack(*(const u32x4_t *)(tile + s.row * kChunkBytes + l16 * 16), f);
+        for (int kk = 0; kk < C::KT / 16; ++kk) {
+            bf16x8_t dl[3][C::EB], xv[C::XP];
 #pragma unroll
-                    for (int q = 0; q < P::N; ++q) v[q] = fmaf(s.dl, f[q], v[q]);
-                }
+            for (int n = 0; n < 3; ++n)
+#pragma unroll
+                for (int i = 0; i < C::EB; ++i)
+                    dl[n][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(smem + n * C::DPLANE + (e0 + i * 32 + (lane & 31)) * C::DROW + (kk * 16 + 8 * (lane >> 5)) * 2));
+#pragma unroll
+            for (int n = 0; n < C::XP; ++n) {
+                const char *p = xs + n * C::XPLANE + (kk * 16 + 8 * (lane >> 5) + ((lane & 15) >> 2)) * C::XROW + (c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)p);
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(p + 4 * C::XROW));
+                xv[n] = __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
-            sum_groups<P::N>(v);
+            // the smallest products first; those below 2^-24 of the largest are left out
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) acc[n][i] += v[i];
-            vb += __shfl_xor(vb, 16);
-            vb += __shfl_xor(vb, 32);
-            if (lane == n) bias += vb;
-            __builtin_amdgcn_sched_barrier(0);  // (or the loops' loads are drawn together, and registers spilled for them)
+            for (int order = 2; order >= 0; --order)
+#pragma unroll
+                for (int n = 0; n < C::XP && n <= order; ++n)
+#pragma unroll
+                    for (int i = 0; i < C::EB; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - n][i], xv[n], acc[i], 0, 0, 0);
         }
+    };
+    for (int t0 = t_begin; t0 < t_end; t0 += XD * C::KT) {
+#pragma unroll
+        for (int i = 0; i < XD; ++i)
+            if (t0 + i * C::KT < t_end) block(t0 + i * C::KT, rows[i], slots[i % SD]);
     }
-    float *out = a.dWg ? a.dWg + part * a.part_stride : nullptr, *out_bias = a.dbias ? a.dbias + part * a.part_stride : nullptr;
-    if (const int e = wave + lane * kGateGradWaves; out_bias && chunk == 0 && e < a.E) out_bias[e] = bias;
-    if (!a.x) return;
-    // [COLS][E] in pieces of 32 columns through LDS, so that rows of dWg are stored whole
-    float *turn = (float *)smem;
-    const int my_col = l16 * P::N + (lane >> 5) * (P::N / 2) + (group & 1) * (P::N / 4), stride = a.E + 1;
-    for (int c0 = 0; c0 < COLS && col0 + c0 < a.d; c0 += 32) {
-        __syncthreads();
-        if (my_col >= c0 && my_col < c0 + 32) {
+    float *out = a.dw_parts == 1 ? a.dWg : a.parts + part * a.part_stride;
+    // a lane has column lane % 32 of a block, and experts 8 q + 4 (lane / 32) .. + 3
+    if (const int col = col0 + c0 + (lane & 31); col < a.d) {
 #pragma unroll
-            for (int n = 0; n < NE; ++n)
-                if (const int e = wave + n * kGateGradWaves; e < a.E) {
+        for (int i = 0; i < C::EB; ++i)
 #pragma unroll
-                    for (int i = 0; i < KEEP; ++i) turn[(my_col - c0 + i) * stride + e] = acc[n][i];
+            for (int q = 0; q < 4; ++q) {
+                const int e = e0 + i * 32 + 8 * q + 4 * (lane >> 5);
+                float *to = out + (size_t)col * a.E + e;
+                const f32x16_t &v = acc[i];
+                if (a.E % 4 == 0) {
+                    if (e < a.E) *(f32x4_t *)to = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        if (e + n < a.E) to[n] = v[4 * q + n];
                 }
-        }
-        __syncthreads();
-        const int n_out = min(32, a.d - col0 - c0) * a.E;
-        for (int i = tid; i < n_out; i += kGateGradThreads) {
-            const int c = i / a.E;
-            out[(size_t)(col0 + c0) * a.E + i] = turn[c * stride + i - c * a.E];
-        }
+            }
+    }
+    sync_stores();
+    if (odd[1] < 0) return;
+    // numbers of x that are not finite: a column's one after the other
+    const int col = col0 + tid;
+    if (tid >= C::COLS || col >= a.d) return;
+    for (int t = odd[0]; t <= odd[1]; ++t) {
+        const float v = Elem<ET>::load((const ET *)a.x, (size_t)t * a.d + col);
+        if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) continue;
+        const size_t s = (size_t)t * a.k;
+        float mean = 0.f;
+        for (int j = 0; j < a.k; ++j) mean += a.w[s + j] * a.dw[s + j];
+        for (int j = 0; j < a.k; ++j)
+            if ((u32)a.idx[s + j] < (u32)a.E) out[(size_t)col * a.E + a.idx[s + j]] += v * (a.w[s + j] * (a.dw[s + j] - mean));
     }
 }
 
-template <typename ET, int NE>
-__global__ __launch_bounds__(kGateGradThreads) void k_gate_grad(GateGradArgs a) {
+// dbias over the tokens of a part: the lanes that take a token have sums of their own in LDS, since two tokens may choose the same expert.
+__device__ __forceinline__ void gate_bias_task(const GateGradArgs &a, char *smem, int part) {
+    const int log2 = gate_lanes_log2(a.k), groups = kGateGradThreads >> log2;
+    const int tid = threadIdx.x, group = tid >> log2;
+    float *sums = (float *)smem, *mine = sums + group * a.E;  // [groups][E]
+    const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
+    for (int i = tid; i < groups * a.E; i += kGateGradThreads) sums[i] = 0.f;
+    __syncthreads();
+    for (int t0 = t_begin; t0 < t_end; t0 += groups) {
+        GateSlots<1> slots;
+        slots.load(a, log2, t0, min(groups, t_end - t0));
+        slots.finish(a, log2, min(groups, t_end - t0), [&](int, int, int, int e, float dl) {
+            if (e >= 0) mine[e] += dl;
+        });
+    }
+    __syncthreads();
+    if (tid >= a.E) return;
+    float sum = 0.f;
+    for (int g = 0; g < groups; ++g) sum += sums[g * a.E + tid];
+    (a.dw_parts == 1 ? a.dbias : a.parts + part * a.part_stride + (size_t)a.d * a.E)[tid] = sum;
+}
+
+template <class C>
+__global__ __launch_bounds__(kGateGradThreads, 4) void k_gate_grad(GateGradArgs a) {
     extern __shared__ __align__(16) char smem[];
-    const int n_dw = a.dw_chunks * a.dw_parts;
-    if ((int)blockIdx.x < n_dw)
-        gate_dw_task<ET, NE>(a, smem, blockIdx.x % a.dw_chunks, blockIdx.x / a.dw_chunks);
+    // dWg's tasks, dbias's, then dx's
+    const int n_w = a.dw_chunks * a.dw_parts, n_b = n_w + (a.dbias ? a.dw_parts : 0), task = blockIdx.x;
+    if (task < n_w)
+        gate_dw_task<C>(a, smem, task % a.dw_chunks, task / a.dw_chunks);
+    else if (task < n_b)
+        gate_bias_task(a, smem, task - n_w);
     else
-        gate_dx_task<ET>(a, smem, (blockIdx.x - n_dw) % a.chunks, (blockIdx.x - n_dw) / a.chunks);
+        gate_dx_task<typename C::ET>(a, smem, (task - n_b) % a.dx_chunks, (task - n_b) / a.dx_chunks);
 }
 
-// The parts' sums, added up part by part: n sums each, the first n_w of them dWg's.
-static __global__ __launch_bounds__(kThreads) void k_gate_grad_join(const float *parts, size_t stride, int n_parts, size_t from, size_t n_w, size_t n, float *dWg, float *dbias) {
-    for (size_t i = from + blockIdx.x * (size_t)kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) {
+// The parts' sums added up, part by part: dWg's d E (whole pieces of 4), then dbias's E.
+static __global__ __launch_bounds__(kThreads) void k_gate_grad_join(GateGradArgs a) {
+    const size_t n = (size_t)a.d * a.E / 4, i = blockIdx.x * (size_t)kThreads + threadIdx.x;
+    if (i < n) {
+        if (!a.dWg) return;
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int p = 0; p < a.dw_parts; ++p) sum += *(const f32x4_t *)(a.parts + p * a.part_stride + i * 4);
+        *(f32x4_t *)(a.dWg + i * 4) = sum;
+    } else if (a.dbias && i - n < (size_t)a.E) {
         float sum = 0.f;
-        for (int p = 0; p < n_parts; ++p) sum += parts[p * stride + i];
-        if (i < n_w)
-            dWg[i] = sum;
-        else
-            dbias[i - n_w] = sum;
+        for (int p = 0; p < a.dw_parts; ++p) sum += a.parts[p * a.part_stride + n * 4 + (i - n)];
+        a.dbias[i - n] = sum;
     }
 }
 

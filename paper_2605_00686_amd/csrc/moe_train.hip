@@ -19,39 +19,34 @@ static unsigned grid_for(size_t n, size_t each) {
     return (unsigned)(g < (1u << 20) ? g : (1u << 20));
 }
 
-static size_t gate_grad_stride(const moe_problem_t *p) { return ((size_t)p->d * p->E + p->E + 63) / 64 * 64; }  // floats of a part
-
-// How the gate's gradient is cut: blocks of tokens, and parts of the tokens for tasks of dWg and of dx.
+// How the gate's gradient is cut.
 static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int cols = kChunkBytes / elem_bytes(p);
     a->T = p->T; a->d = p->d; a->E = p->E; a->k = p->k;
-    a->block = p->k <= 8 ? 256 : p->k <= 16 ? 128 : 64;
-    a->chunks = (p->d + cols - 1) / cols;
-    const int blocks = (p->T + a->block - 1) / a->block;
-    int want = 256 / a->chunks;
-    if (want < 1) want = 1;
-    if (want > blocks) want = blocks;
-    a->dw_blocks = a->dx_blocks = (blocks + want - 1) / want;
-    a->dw_parts = a->dx_parts = (blocks + a->dw_blocks - 1) / a->dw_blocks;
+    a->dx_chunks = (p->d + cols - 1) / cols;
+    a->block = p->k <= 8 ? 128 : p->k <= 16 ? 64 : 32;
+    const auto parts_of = [](int tasks, int chunks) { return tasks > chunks ? tasks / chunks : 1; };
+    const int blocks = (p->T + a->block - 1) / a->block, dx_want = parts_of(512, a->dx_chunks);
+    a->dx_blocks = (blocks + dx_want - 1) / dx_want;
+    a->dx_parts = (blocks + a->dx_blocks - 1) / a->dx_blocks;
+    constexpr int kReduction = 64;  // tokens, a multiple of every shape's
+    const int dw_want = parts_of(256, (p->d + kGateDwCols - 1) / kGateDwCols);
+    a->dw_tokens = ((p->T + dw_want - 1) / dw_want + kReduction - 1) / kReduction * kReduction;
+    a->dw_parts = (p->T + a->dw_tokens - 1) / a->dw_tokens;
+    a->part_stride = ((size_t)p->d * p->E + p->E + 63) / 64 * 64;
 }
 
-template <typename ET>
+template <class C>
 static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
-    const size_t rows = (size_t)(a.dw_parts && a.x ? a.block : 0), columns = a.dx_parts ? a.E : 0;
-    size_t smem = sizeof(GateGradLds) + (rows > columns ? rows : columns) * kChunkBytes;
-    const size_t turn = (size_t)32 * (a.E + 1) * 4;
-    if (smem < turn) smem = turn;
-    const dim3 grid(a.dw_chunks * a.dw_parts + a.chunks * a.dx_parts), block(kGateGradThreads);
-    auto go = [&](auto kern) {
-        if (const int rc = allow_lds((const void *)kern, smem)) return rc;
-        hipLaunchKernelGGL(kern, grid, block, smem, st, a);
-        return launched();
-    };
-    const int per_wave = (a.E + kGateGradWaves - 1) / kGateGradWaves;
-    if (per_wave <= 1) return go(k_gate_grad<ET, 1>);
-    if (per_wave <= 4) return go(k_gate_grad<ET, 4>);
-    if (per_wave <= 8) return go(k_gate_grad<ET, 8>);
-    return go(k_gate_grad<ET, 16>);
+    const size_t dx = a.dx_parts ? sizeof(GateDxLds) + (size_t)(a.E + 1) * kChunkBytes : 0;
+    const size_t dw = a.dw_chunks ? (size_t)C::LDS : 0, db = a.dbias ? (size_t)kGateGradThreads / 8 * a.E * 4 : 0;
+    const size_t smem = dx > dw ? (dx > db ? dx : db) : (dw > db ? dw : db);
+    if (const int rc = allow_lds((const void *)k_gate_grad<C>, smem)) return rc;
+    hipLaunchKernelGGL(k_gate_grad<C>, dim3((a.dw_chunks + (a.dbias ? 1 : 0)) * a.dw_parts + a.dx_chunks * a.dx_parts), dim3(kGateGradThreads), smem, st, a);
+    if (const int rc = launched()) return rc;
+    if (a.dw_parts <= 1) return MOE_OK;
+    hipLaunchKernelGGL(k_gate_grad_join, dim3((unsigned)(((size_t)a.d * a.E / 4 + a.E + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a);
+    return launched();
 }
 
 extern "C" {
@@ -104,12 +99,12 @@ size_t moe_backward_workspace_bytes(const moe_problem_t *p) {
     if (check_problem(p) != MOE_OK) return 0;
     GateGradArgs a;
     gate_grad_plan(p, &a);
-    return a.dw_parts * gate_grad_stride(p) * 4;
+    return a.dw_parts * a.part_stride * 4;
 }
 
 int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx, const float *topk_w,
                        const float *dtopk_w, void *dx, float *dWg, float *dgate_bias, int32_t *status_dev, void *workspace, void *stream) {
-    int rc = check_problem(p);
+    const int rc = check_problem(p);
     if (rc) return rc;
     if (!topk_idx || !topk_w || !dtopk_w || (!dx && !dWg && !dgate_bias)) return MOE_ERR_INVALID_ARG;
     if ((dx && !Wg) || (dWg && !x)) return MOE_ERR_INVALID_ARG;
@@ -120,22 +115,13 @@ int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, co
     gate_grad_plan(p, &a);
     a.x = dWg ? x : nullptr; a.Wg = Wg; a.idx = topk_idx; a.w = topk_w; a.dw = dtopk_w; a.dx = dx; a.dWg = dWg; a.dbias = dgate_bias;
     a.status = status_dev;
-    a.dw_chunks = dWg ? a.chunks : 1;
+    a.dw_chunks = dWg ? (p->d + kGateDwCols - 1) / kGateDwCols : 0;
     if (!sums) a.dw_parts = 0;
     if (!dx) a.dx_parts = 0;
-    const size_t n_w = (size_t)p->d * p->E;
-    if (a.dw_parts > 1) {
-        a.part_stride = gate_grad_stride(p);
-        if (dWg) a.dWg = (float *)workspace;
-        if (dgate_bias) a.dbias = (float *)workspace + n_w;
-    }
+    a.parts = (float *)workspace;
     hipStream_t st = (hipStream_t)stream;
-    rc = p->dtype == MOE_DT_F32 ? launch_gate_grad<float>(a, st) : launch_gate_grad<bf16_t>(a, st);
-    if (rc || a.dw_parts <= 1) return rc;
-    const size_t from = dWg ? 0 : n_w, n = dgate_bias ? n_w + p->E : n_w;
-    hipLaunchKernelGGL(k_gate_grad_join, dim3(grid_for(n - from, kThreads)), dim3(kThreads), 0, st, (const float *)workspace, a.part_stride,
-                       a.dw_parts, from, n_w, n, dWg, dgate_bias);
-    return launched();
+    if (p->dtype == MOE_DT_F32) return p->E <= 128 ? launch_gate_grad<GateDw32M>(a, st) : launch_gate_grad<GateDw32L>(a, st);
+    return p->E <= 128 ? launch_gate_grad<GateDw16M>(a, st) : launch_gate_grad<GateDw16L>(a, st);
 }
 
 static int check_swiglu(const moe_problem_t *p, int64_t ld, const int32_t *counts, const void *codes, const void *scales) {

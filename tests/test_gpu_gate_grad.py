@@ -198,3 +198,27 @@ def test_other_stream_and_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, outs))
         go()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,d,E,k,dtype", [(300, 192, 12, 3, "bf16"), (200, 80, 140, 4, "f32"), (70, 320, 70, 2, "bf16"), (500, 128, 200, 2, "bf16")])
+def test_not_finite_inputs_reach_the_chosen_experts_and_tokens_only(T, d, E, k, dtype):
+    B, p, gen, dt, idx, w, dw, x, Wg = make(T, d, E, k, dtype)
+    odd = [(3, 5, float("inf")), (3, 6, float("nan")), (T - 1, d - 1, float("-inf")), (T // 2, 5, float("nan"))]
+    clean = x.clone()
+    for t, c, v in odd:
+        x[t, c], clean[t, c] = v, 0.0
+    odd_e = int(idx[1, 0])
+    Wg[7, odd_e] = float("inf")
+    dx, dWg, db = (t.cpu() for t in call(B, p, x, Wg, idx, w, dw))
+    # dx: column 7 of the tokens that chose the expert
+    bad = torch.zeros(T, d, dtype=torch.bool)
+    bad[(idx == odd_e).any(1), 7] = True
+    assert torch.equal(~torch.isfinite(dx), bad)
+    # dWg: the columns of x at hand, of the token's experts; everything else as if those numbers were zero
+    bad = torch.zeros(d, E, dtype=torch.bool)
+    for t, c, v in odd:
+        bad[c, idx[t].long()] = True
+    assert torch.equal(~torch.isfinite(dWg), bad)
+    (_, _), (ref, bound), (ref_b, bound_b) = expected(idx, w, dw, clean, torch.zeros_like(Wg), dt)
+    assert bool(((dWg.double() - ref).abs() <= bound)[~bad].all())
+    assert bool(((db.double() - ref_b).abs() <= bound_b).all())
