@@ -66,9 +66,8 @@ struct GateSlots {
         const int j = threadIdx.x & ((1 << log2) - 1);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (skip(i, log2, n)) continue;
             const int t = (threadIdx.x + i * kGateGradThreads) >> log2;
-            const bool in = t < n && j < a.k;
+            const bool in = t < n && j < a.k;  // (else the first slot of all: no load is conditional)
             const u32 s = in ? (u32)(t0 + t) * (u32)a.k + j : 0u;  // (T k is at most 2^30)
             w[i] = a.w[s], dw[i] = a.dw[s], e[i] = a.idx[s];
             if (!in) w[i] = dw[i] = 0.f;
@@ -162,39 +161,34 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
     }
 }
 
-// A finite fp32 number as three bf16 numbers (their bits), 8 bits of it each; one that is not: itself and zeros.
+// A finite fp32 number as three bf16 numbers in the upper halves, 8 bits of it each (an infinity becomes one and two NaNs).
 __device__ __forceinline__ void cut3(float v, u32 *b) {
-    const u32 h = __float_as_uint(v) & 0xffff0000u;
-    const float r = v - __uint_as_float(h);
-    const u32 m = __float_as_uint(r) & 0xffff0000u;
-    const float s = r - __uint_as_float(m);
-    const bool finite = (h & 0x7f800000u) != 0x7f800000u;
-    // (a NaN keeps a bit that survives the cut)
-    b[0] = finite ? h >> 16 : (__float_as_uint(v) >> 16) | ((__float_as_uint(v) & 0x7fffffu) ? 0x40u : 0u);
-    b[1] = finite ? m >> 16 : 0u;
-    b[2] = finite ? __float_as_uint(s) >> 16 : 0u;
+    b[0] = __float_as_uint(v) & 0xffff0000u;
+    const float r = v - __uint_as_float(b[0]);
+    b[1] = __float_as_uint(r) & 0xffff0000u;
+    b[2] = __float_as_uint(r - __uint_as_float(b[1]));
 }
 
-// Shape of a dWg task: 8 wavefronts as 4 x 2, each with EB blocks of 32 experts x 32 columns; KT tokens per reduction block.
-template <typename ET_, int EB_, int KT_>
+// Shape of a dWg task: KT tokens per reduction block, of which either half of the 8 wavefronts multiplies one half; a wavefront has EB
+// blocks of 32 experts and all columns.  (What a step reads from LDS bounds it: three pieces of dl per block of 32 experts, so every
+// wavefront uses them on 64 columns.)
+template <typename ET_, int EB_, int KT_, int PER_>
 struct GateDwShape {
     using ET = ET_;
-    static constexpr int EB = EB_, KT = KT_, WE = 4, COLS = kGateDwCols, EPAD = EB * WE * 32;
+    static constexpr int EB = EB_, KT = KT_, WE = 4, COLS = kGateDwCols, CB = COLS / 32, EPAD = EB * WE * 32;
     static constexpr int XP = sizeof(ET) == 4 ? 3 : 1;  // bf16 numbers that make up one of x
     // Rows of LDS.  dl, [3][EPAD][KT] bf16: 16 bytes behind each row, so that 16 lanes' pieces of 16 bytes meet no bank twice; x,
     // [XP][KT][COLS] bf16: rows 16 banks apart modulo 64, for the transposing read of 4 rows x 64 bytes.
     static constexpr int DROW = KT * 2 + 16, XROW = COLS * 2 + 64;
     static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
-    static constexpr int O_X = 3 * DPLANE, O_ODD = O_X + XP * XPLANE, LDS = O_ODD + 16;
-    static constexpr int PER = KT * 32 / kGateGradThreads;        // slots of a reduction block per thread, at most
-    static constexpr int LANES = COLS / Piece<ET>::N;             // of a row of x, a piece each
-    static_assert(KT * LANES <= kGateGradThreads, "a piece per thread");
+    static constexpr int O_X = 3 * DPLANE, TURN = COLS * (EPAD + 4) * 4;
+    static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + 16;
+    static constexpr int WAVES = XP * EB > 3 ? 2 : 4;  // on a SIMD; the largest takes more registers than two workgroups of a CU have
+    static constexpr int GROUP = PER_ == 1 ? 2 : 1;  // blocks whose numbers are loaded together
+    static constexpr int PER = PER_;                   // passes over the slots of a reduction block
+    static constexpr int LANES = COLS / Piece<ET>::N;  // of a row of x, a piece each
+    static constexpr int NX = (KT * LANES + kGateGradThreads - 1) / kGateGradThreads, XSTEP = kGateGradThreads / LANES;  // pieces per thread, tokens apart
 };
-using GateDw16M = GateDwShape<bf16_t, 1, 64>;  // up to 128 experts
-using GateDw16L = GateDwShape<bf16_t, 2, 32>;  // 256
-using GateDw32M = GateDwShape<float, 1, 32>;
-using GateDw32L = GateDwShape<float, 2, 32>;
-
 // dWg[columns of a chunk, :] over the tokens of a part.  For a reduction block of tokens dl
 // lies dense in LDS, by expert: its slots are written there, multiplied, and cleared again.
 template <class C>
@@ -208,137 +202,196 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
     char *xs = smem + C::O_X;
     int *odd = (int *)(smem + C::O_ODD);  // first and last token whose x has a number here that is not finite
-    // Loads run four blocks ahead (x) and two (slots): a block's tokens are few, and a CU may have one workgroup
-    constexpr int XD = 4, SD = 2;
-    u32x4_t rows[XD];
-    GateSlots<C::PER> slots[SD];
-    const int x_tok = tid / C::LANES, x_lane = tid % C::LANES;
+    // Loads run a group of blocks ahead, whole groups at a time: a block's tokens are few, and a CU may have one workgroup
+    constexpr int GROUP = C::GROUP;
+    u32x4_t rows[GROUP][C::NX];
+    GateSlots<C::PER> slots[GROUP];
+    const int x_tok = tid / C::LANES % C::KT, x_lane = tid % C::LANES;
+    const bool x_mine = tid < C::KT * C::LANES;
     const ET *x = (const ET *)a.x + min(col0 + x_lane * P::N, a.d - P::N);
-    auto load_x = [&](u32x4_t &v, int t0) {
-        if (t0 < t_end && x_tok < C::KT) v = *(const u32x4_t *)(x + (size_t)min(t0 + x_tok, t_end - 1) * a.d);
+    // (no load is conditional: the number of loads in flight is then known at every wait)
+    auto load_x = [&](u32x4_t(&v)[C::NX], int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < C::NX; ++n) v[n] = *(const u32x4_t *)(x + (size_t)min(t0 + x_tok + n * C::XSTEP, t_end - 1) * a.d);
     };
+    auto load_group = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < SD; ++i) slots[i].load(a, log2, t_begin + i * C::KT, min(C::KT, t_end - t_begin - i * C::KT));
+        for (int i = 0; i < GROUP; ++i) slots[i].load(a, log2, t0 + i * C::KT, min(C::KT, t_end - t0 - i * C::KT));
 #pragma unroll
-    for (int i = 0; i < XD; ++i) load_x(rows[i], t_begin + i * C::KT);
+        for (int i = 0; i < GROUP; ++i) load_x(rows[i], t0 + i * C::KT);
+    };
+    load_group(t_begin);
     for (int i = tid * 16; i < C::O_X; i += kGateGradThreads * 16) *(u32x4_t *)(smem + i) = u32x4_t{0, 0, 0, 0};
     if (tid == 0) odd[0] = 0x7fffffff, odd[1] = -1;
-    const int we = wave % C::WE, wc = wave / C::WE, e0 = we * C::EB * 32, c0 = wc * 32;
-    f32x16_t acc[C::EB];
+    const int half = wave / C::WE, e0 = wave % C::WE * C::EB * 32;
+    f32x16_t acc[C::EB][C::CB];
 #pragma unroll
     for (int i = 0; i < C::EB; ++i)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][q] = 0.f;
-    auto put_x = [&](u32x4_t v, int t0) {
-        if (x_tok >= C::KT) return;
-        const bool in = t0 + x_tok < t_end;
-        bool strange = false;
-        if constexpr (sizeof(ET) == 2) {
-            u32 carry = 0u;  // of exponents that are all ones
+        for (int j = 0; j < C::CB; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                v[q] = in ? v[q] : 0u;
-                carry |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-            }
-            strange = carry != 0u;
-            if (strange) {
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+    // A block's numbers on their way from memory to LDS: this thread's piece of x as bf16 numbers, and its slots
+    uint2 piece[C::NX][sizeof(ET) == 2 ? 2 : 3];
+    int at[C::PER], old[C::PER];  // where its slots lie in dl, -1 = it has none; and those of the block before
+    u32 cut[C::PER][3];
+#pragma unroll
+    for (int i = 0; i < C::PER; ++i) at[i] = old[i] = -1;
+    auto prepare = [&](int t0, u32x4_t(&row)[C::NX], GateSlots<C::PER> &slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < C::NX; ++m) {
+            u32x4_t v = row[m];
+            bool strange = false;
+            if constexpr (sizeof(ET) == 2) {
+                u32 carry = 0u;  // of exponents that are all ones
+#pragma unroll
+                for (int q = 0; q < 4; ++q) carry |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                strange = carry != 0u;
+                if (strange) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
+                        if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
+                    }
+                }
+                piece[m][0] = uint2{v[0], v[1]}, piece[m][1] = uint2{v[2], v[3]};
+            } else {
+                u32 b[4][3];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
-                    if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
+                    const bool fine = (v[q] & 0x7f800000u) != 0x7f800000u;
+                    strange |= !fine;
+                    cut3(fine ? __uint_as_float(v[q]) : 0.f, b[q]);
                 }
-            }
-            *(u32x4_t *)(xs + x_tok * C::XROW + x_lane * 16) = v;
-        } else {
-            u32 b[4][3];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const bool fine = (v[q] & 0x7f800000u) != 0x7f800000u;
-                strange |= !fine;
-                cut3(in && fine ? __uint_as_float(v[q]) : 0.f, b[q]);
+                for (int n = 0; n < 3; ++n) piece[m][n] = uint2{(b[0][n] >> 16) | (b[1][n] & 0xffff0000u), (b[2][n] >> 16) | (b[3][n] & 0xffff0000u)};
             }
-#pragma unroll
-            for (int n = 0; n < 3; ++n)
-                *(uint2 *)(xs + n * C::XPLANE + x_tok * C::XROW + x_lane * 8) = uint2{b[0][n] | (b[1][n] << 16), b[2][n] | (b[3][n] << 16)};
+            if (const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1); strange) atomicMin(&odd[0], t), atomicMax(&odd[1], t);
         }
-        if (strange && in) atomicMin(&odd[0], t0 + x_tok), atomicMax(&odd[1], t0 + x_tok);
-    };
-    int at[C::PER];  // where this thread's slots lie in dl, -1 = it has none
 #pragma unroll
-    for (int i = 0; i < C::PER; ++i) at[i] = -1;
-    auto block = [&](int t0, u32x4_t &row, GateSlots<C::PER> &slot) {
-        __syncthreads();  // (the block before is done with the LDS)
-#pragma unroll
-        for (int i = 0; i < C::PER; ++i)
-            if (!GateSlots<C::PER>::skip(i, log2, C::KT) && at[i] >= 0) {
-#pragma unroll
-                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = 0;
-                at[i] = -1;
-            }
-        put_x(row, t0);
-        load_x(row, t0 + XD * C::KT);
-        u32 cut[C::PER][3];
+        for (int i = 0; i < C::PER; ++i) old[i] = at[i], at[i] = -1;
         slot.finish(a, log2, min(C::KT, t_end - t0), [&](int i, int t, int, int e, float dl) {
             at[i] = e < 0 ? -1 : e * C::DROW + t * 2;
             cut3(dl, cut[i]);
         });
-        slot.load(a, log2, t0 + SD * C::KT, min(C::KT, t_end - t0 - SD * C::KT));
-        __syncthreads();
+    };
+    auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < C::PER; ++i)
-            if (!GateSlots<C::PER>::skip(i, log2, C::KT) && at[i] >= 0) {
+        for (int n = 0; n < C::KT / 32; ++n) {
+            const int kk = half * (C::KT / 32) + n;
+            bf16x8_t dl[3][C::EB], xv[C::XP][C::CB];
 #pragma unroll
-                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)cut[i][n];
-            }
-        __syncthreads();
-        if (e0 >= a.E) return;
-#pragma unroll
-        for (int kk = 0; kk < C::KT / 16; ++kk) {
-            bf16x8_t dl[3][C::EB], xv[C::XP];
-#pragma unroll
-            for (int n = 0; n < 3; ++n)
+            for (int c = 2; c >= 0; --c)
 #pragma unroll
                 for (int i = 0; i < C::EB; ++i)
-                    dl[n][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(smem + n * C::DPLANE + (e0 + i * 32 + (lane & 31)) * C::DROW + (kk * 16 + 8 * (lane >> 5)) * 2));
+                    dl[c][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(smem + c * C::DPLANE + (e0 + i * 32 + (lane & 31)) * C::DROW + (kk * 16 + 8 * (lane >> 5)) * 2));
 #pragma unroll
-            for (int n = 0; n < C::XP; ++n) {
-                const char *p = xs + n * C::XPLANE + (kk * 16 + 8 * (lane >> 5) + ((lane & 15) >> 2)) * C::XROW + (c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)p);
-                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(p + 4 * C::XROW));
-                xv[n] = __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+            for (int c = 0; c < C::XP; ++c)
+#pragma unroll
+                for (int j = 0; j < C::CB; ++j) {
+                    const char *p = xs + c * C::XPLANE + (kk * 16 + 8 * (lane >> 5) + ((lane & 15) >> 2)) * C::XROW + (j * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)p);
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(p + 4 * C::XROW));
+                    xv[c][j] = __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
             // the smallest products first; those below 2^-24 of the largest are left out
 #pragma unroll
             for (int order = 2; order >= 0; --order)
 #pragma unroll
-                for (int n = 0; n < C::XP && n <= order; ++n)
+                for (int c = 0; c < C::XP && c <= order; ++c)
 #pragma unroll
-                    for (int i = 0; i < C::EB; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - n][i], xv[n], acc[i], 0, 0, 0);
+                    for (int i = 0; i < C::EB; ++i)
+#pragma unroll
+                        for (int j = 0; j < C::CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - c][i], xv[c][j], acc[i][j], 0, 0, 0);
         }
     };
-    for (int t0 = t_begin; t0 < t_end; t0 += XD * C::KT) {
+    // The block at t0, whose numbers are prepared; `after` prepares the next one's.  The halves of the wavefronts, one of each on a
+    // SIMD, prepare before and after they multiply: one's vector instructions run beside the other's products.
+    auto block = [&](auto after) __attribute__((always_inline)) {
+        __syncthreads();  // (the block before is done with the LDS)
 #pragma unroll
-        for (int i = 0; i < XD; ++i)
-            if (t0 + i * C::KT < t_end) block(t0 + i * C::KT, rows[i], slots[i % SD]);
+        for (int i = 0; i < C::PER; ++i)
+            if (old[i] >= 0) {
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + old[i]) = 0;
+            }
+        if (x_mine) {
+#pragma unroll
+            for (int m = 0; m < C::NX; ++m) {
+                char *to = xs + (x_tok + m * C::XSTEP) * C::XROW;
+                if constexpr (sizeof(ET) == 2)
+                    *(u32x4_t *)(to + x_lane * 16) = u32x4_t{piece[m][0].x, piece[m][0].y, piece[m][1].x, piece[m][1].y};
+                else
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) *(uint2 *)(to + n * C::XPLANE + x_lane * 8) = piece[m][n];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i)
+            if (at[i] >= 0) {
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)(cut[i][n] >> 16);
+            }
+        __syncthreads();
+        if (half == 0) after();
+        if (e0 < a.E) multiply();
+        if (half == 1) after();
+    };
+    __syncthreads();  // (`odd` is set)
+    for (int t0 = t_begin; t0 < t_end; t0 += GROUP * C::KT) {
+        u32x4_t x_now[GROUP][C::NX];
+        GateSlots<C::PER> slots_now[GROUP];
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            slots_now[i] = slots[i];
+#pragma unroll
+            for (int n = 0; n < C::NX; ++n) x_now[i][n] = rows[i][n];
+        }
+        load_group(t0 + GROUP * C::KT);
+        prepare(t0, x_now[0], slots_now[0]);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            if (t0 + i * C::KT >= t_end) break;
+            block([&]() __attribute__((always_inline)) {
+                if (i + 1 < GROUP) prepare(t0 + (i + 1) * C::KT, x_now[(i + 1) % GROUP], slots_now[(i + 1) % GROUP]);
+            });
+        }
     }
     float *out = a.dw_parts == 1 ? a.dWg : a.parts + part * a.part_stride;
-    // a lane has column lane % 32 of a block, and experts 8 q + 4 (lane / 32) .. + 3
-    if (const int col = col0 + c0 + (lane & 31); col < a.d) {
+    // A lane has column lane % 32 of a block, and experts 8 q + 4 (lane / 32) .. + 3.  Through LDS, so that memory sees the chunk's rows of
+    // dWg, which lie one behind the other, in one piece.
+    const int stride = C::EPAD + 4;
+    float *turn = (float *)smem;
+    auto mine = [&](int i, int j, int q) {
+        const f32x16_t &v = acc[i][j];
+        return f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    };
+    for (int h = 1; h >= 0; --h) {  // one half's sums, then the other's added to them
+        __syncthreads();
+        if (half != h) continue;
 #pragma unroll
         for (int i = 0; i < C::EB; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int e = e0 + i * 32 + 8 * q + 4 * (lane >> 5);
-                float *to = out + (size_t)col * a.E + e;
-                const f32x16_t &v = acc[i];
-                if (a.E % 4 == 0) {
-                    if (e < a.E) *(f32x4_t *)to = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-                } else {
+            for (int j = 0; j < C::CB; ++j)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
-                        if (e + n < a.E) to[n] = v[4 * q + n];
+                for (int q = 0; q < 4; ++q) {
+                    f32x4_t &to = *(f32x4_t *)(turn + (j * 32 + (lane & 31)) * stride + e0 + i * 32 + 8 * q + 4 * (lane >> 5));
+                    to = h ? mine(i, j, q) : to + mine(i, j, q);
                 }
-            }
+    }
+    __syncthreads();
+    const int n_out = min(C::COLS, a.d - col0) * a.E, step = a.E % 4 == 0 ? 4 : 1;
+    float *to = out + (size_t)col0 * a.E;
+    int c = tid * step / a.E, e = tid * step - c * a.E;
+    const int dc = kGateGradThreads * step / a.E, de = kGateGradThreads * step - dc * a.E;
+    for (int i = tid * step; i < n_out; i += kGateGradThreads * step) {
+        if (step == 4)
+            *(f32x4_t *)(to + i) = *(const f32x4_t *)(turn + c * stride + e);
+        else
+            to[i] = turn[c * stride + e];
+        c += dc, e += de;
+        if (e >= a.E) e -= a.E, ++c;
     }
     sync_stores();
     if (odd[1] < 0) return;
@@ -379,7 +432,7 @@ __device__ __forceinline__ void gate_bias_task(const GateGradArgs &a, char *smem
 }
 
 template <class C>
-__global__ __launch_bounds__(kGateGradThreads, 4) void k_gate_grad(GateGradArgs a) {
+__global__ __launch_bounds__(kGateGradThreads, C::WAVES) void k_gate_grad(GateGradArgs a) {
     extern __shared__ __align__(16) char smem[];
     // dWg's tasks, dbias's, then dx's
     const int n_w = a.dw_chunks * a.dw_parts, n_b = n_w + (a.dbias ? a.dw_parts : 0), task = blockIdx.x;

@@ -29,9 +29,22 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int blocks = (p->T + a->block - 1) / a->block, dx_want = parts_of(512, a->dx_chunks);
     a->dx_blocks = (blocks + dx_want - 1) / dx_want;
     a->dx_parts = (blocks + a->dx_blocks - 1) / a->dx_blocks;
+    // Parts of dWg: a reduction block takes a task 1 us (64 tokens, or 32 beyond 128 experts), a part's sums 0.6 us per MB to write and read
+    // again, and the launch that adds them up 3 us.  At most one task per CU: two share it, and the sums of twice as many parts cost more
+    // than that gains.  us, 4096 x 8 of 128 of 2048, parts 4 / 8 / 16: 24.3 / 20.5 / 25.3; 2048 x 8 of 256 of 7168, 1 / 2 / 4: 63.1 / 40.4
+    // / 36.4, but with dx beside it 64.1 / 42.9 / 46.3; 512 x 8 of 128 of 2048, 1 / 8: @@ / 12.7.
     constexpr int kReduction = 64;  // tokens, a multiple of every shape's
-    const int dw_want = parts_of(256, (p->d + kGateDwCols - 1) / kGateDwCols);
-    a->dw_tokens = ((p->T + dw_want - 1) / dw_want + kReduction - 1) / kReduction * kReduction;
+    a->dw_chunks = (p->d + kGateDwCols - 1) / kGateDwCols;
+    const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(256, a->dw_chunks);
+    const double unit_us = p->E > 128 || p->dtype == MOE_DT_F32 ? 2.0 : 1.0, part_us = 0.6e-6 * 4.0 * p->d * p->E;
+    double best = 0.0;
+    int each = units;
+    for (int n = 1; n <= most && n <= units; ++n) {
+        const int per = (units + n - 1) / n;
+        const double us = per * unit_us + n * part_us + (n > 1 ? 3.0 : 0.0);
+        if (n == 1 || us < best) best = us, each = per;
+    }
+    a->dw_tokens = each * kReduction;
     a->dw_parts = (p->T + a->dw_tokens - 1) / a->dw_tokens;
     a->part_stride = ((size_t)p->d * p->E + p->E + 63) / 64 * 64;
 }
@@ -47,6 +60,15 @@ static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
     if (a.dw_parts <= 1) return MOE_OK;
     hipLaunchKernelGGL(k_gate_grad_join, dim3((unsigned)(((size_t)a.d * a.E / 4 + a.E + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a);
     return launched();
+}
+
+// KT tokens per reduction block up to 128 experts, 32 beyond (the LDS that dl takes there); one pass over their slots for up to 8
+// choices, else as many as 32 choices take.
+template <typename ET, int KT>
+static int pick_gate_grad(const GateGradArgs &a, hipStream_t st) {
+    constexpr int MANY = KT * 32 / kGateGradThreads;
+    if (a.E <= 128) return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, 1, KT, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, 1, KT, MANY>>(a, st);
+    return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, 2, 32, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, 2, 32, 2>>(a, st);
 }
 
 extern "C" {
@@ -115,13 +137,12 @@ int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, co
     gate_grad_plan(p, &a);
     a.x = dWg ? x : nullptr; a.Wg = Wg; a.idx = topk_idx; a.w = topk_w; a.dw = dtopk_w; a.dx = dx; a.dWg = dWg; a.dbias = dgate_bias;
     a.status = status_dev;
-    a.dw_chunks = dWg ? (p->d + kGateDwCols - 1) / kGateDwCols : 0;
+    if (!dWg) a.dw_chunks = 0;
     if (!sums) a.dw_parts = 0;
     if (!dx) a.dx_parts = 0;
     a.parts = (float *)workspace;
     hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == MOE_DT_F32) return p->E <= 128 ? launch_gate_grad<GateDw32M>(a, st) : launch_gate_grad<GateDw32L>(a, st);
-    return p->E <= 128 ? launch_gate_grad<GateDw16M>(a, st) : launch_gate_grad<GateDw16L>(a, st);
+    return p->dtype == MOE_DT_F32 ? pick_gate_grad<float, 32>(a, st) : pick_gate_grad<bf16_t, 64>(a, st);
 }
 
 static int check_swiglu(const moe_problem_t *p, int64_t ld, const int32_t *counts, const void *codes, const void *scales) {
