@@ -19,6 +19,46 @@ static unsigned grid_for(size_t n, size_t each) {
     return (unsigned)(g < (1u << 20) ? g : (1u << 20));
 }
 
+template <typename ET, int KB, int U, int G>
+static int launch_unsort(UnsortArgs &a, hipStream_t st) {
+    a.parts = (a.d / Piece<ET>::N + G * U - 1) / (G * U);
+    hipLaunchKernelGGL((k_unsort<ET, KB, U, G>), dim3(grid_for((size_t)a.T * a.parts, kThreads / G)), dim3(kThreads), 0, st, a);
+    return launched();
+}
+template <typename ET>
+static int pick_unsort(UnsortArgs &a, hipStream_t st) {
+    const int pieces = a.d / Piece<ET>::N;
+    if (pieces <= 32) {
+        if (pieces <= 8) return a.k <= 2 ? launch_unsort<ET, 2, 1, 8>(a, st) : launch_unsort<ET, 8, 1, 8>(a, st);
+        if (pieces <= 16) return a.k <= 2 ? launch_unsort<ET, 2, 1, 16>(a, st) : launch_unsort<ET, 8, 1, 16>(a, st);
+        return a.k <= 2 ? launch_unsort<ET, 2, 1, 32>(a, st) : launch_unsort<ET, 8, 1, 32>(a, st);
+    }
+    if (a.k <= 2) return pieces <= 64 ? launch_unsort<ET, 2, 1, 64>(a, st) : pieces <= 128 ? launch_unsort<ET, 2, 2, 64>(a, st) : launch_unsort<ET, 2, 4, 64>(a, st);
+    if (a.k <= 4) return pieces <= 64 ? launch_unsort<ET, 4, 1, 64>(a, st) : launch_unsort<ET, 4, 2, 64>(a, st);
+    return launch_unsort<ET, 8, 1, 64>(a, st);
+}
+
+template <typename ET, int KB, int L>
+static int launch_unsort_backward(UnsortArgs &a, hipStream_t st) {
+    a.token_groups = (int)grid_for(a.T, kThreads / L);
+    const unsigned zero_groups = a.capacity > 0 && a.drows ? grid_for(a.rows, 16) : 0u;
+    hipLaunchKernelGGL((k_unsort_backward<ET, KB, L>), dim3(a.token_groups + zero_groups), dim3(kThreads), 0, st, a);
+    return launched();
+}
+template <typename ET, int L>
+static int pick_unsort_backward(UnsortArgs &a, hipStream_t st) {
+    return a.k <= 2 ? launch_unsort_backward<ET, 2, L>(a, st) : a.k <= 4 ? launch_unsort_backward<ET, 4, L>(a, st) : launch_unsort_backward<ET, 8, L>(a, st);
+}
+template <typename ET>
+static int pick_unsort_backward(UnsortArgs &a, hipStream_t st) {
+    const int pieces = a.d / Piece<ET>::N;
+    if (pieces <= 8) return pick_unsort_backward<ET, 8>(a, st);
+    if (pieces <= 16) return pick_unsort_backward<ET, 16>(a, st);
+    if (pieces <= 32) return pick_unsort_backward<ET, 32>(a, st);
+    if (pieces <= 64) return pick_unsort_backward<ET, 64>(a, st);
+    return pieces <= 128 ? pick_unsort_backward<ET, 128>(a, st) : pick_unsort_backward<ET, 256>(a, st);
+}
+
 // How the gate's gradient is cut.
 static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int cols = kChunkBytes / elem_bytes(p);
@@ -82,39 +122,21 @@ int moe_unsort(const moe_problem_t *p, const void *rows, const int32_t *inv_perm
     UnsortArgs a = {};
     a.T = p->T; a.d = p->d; a.k = p->k; a.rows = rows_of(p);
     a.sorted = rows; a.inv_perm = inv_perm; a.w = topk_w; a.addend = addend; a.out = out; a.status = status_dev;
-    const dim3 grid(grid_for(p->T, 4));
-    hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == MOE_DT_F32)
-        hipLaunchKernelGGL(k_unsort<float>, grid, dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(k_unsort<bf16_t>, grid, dim3(kThreads), 0, st, a);
-    return launched();
+    return p->dtype == MOE_DT_F32 ? pick_unsort<float>(a, (hipStream_t)stream) : pick_unsort<bf16_t>(a, (hipStream_t)stream);
 }
 
 int moe_unsort_backward(const moe_problem_t *p, const void *dout, const void *rows, const int32_t *inv_perm, const float *topk_w,
                         const int32_t *counts, void *drows, float *dtopk_w, int32_t *status_dev, void *stream) {
-    int rc = check_problem(p);
+    const int rc = check_problem(p);
     if (rc) return rc;
     if (!dout || !inv_perm || (!drows && !dtopk_w) || (dtopk_w && !rows)) return MOE_ERR_INVALID_ARG;
     if (p->capacity > 0 && !counts) return MOE_ERR_INVALID_ARG;
     if (!aligned16(dout) || !aligned16(rows) || !aligned16(drows)) return MOE_ERR_INVALID_ARG;
     UnsortArgs a = {};
-    a.T = p->T; a.d = p->d; a.k = p->k; a.rows = rows_of(p); a.capacity = p->capacity; a.E = p->E;
+    a.T = p->T; a.d = p->d; a.k = p->k; a.rows = rows_of(p); a.capacity = p->capacity;
     a.dout = dout; a.sorted = rows; a.inv_perm = inv_perm; a.w = topk_w; a.counts = counts; a.drows = drows; a.dw = dtopk_w;
     a.status = status_dev;
-    hipStream_t st = (hipStream_t)stream;
-    const dim3 grid(grid_for(p->T, 4));
-    if (p->dtype == MOE_DT_F32)
-        hipLaunchKernelGGL(k_unsort_backward<float>, grid, dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(k_unsort_backward<bf16_t>, grid, dim3(kThreads), 0, st, a);
-    if ((rc = launched())) return rc;
-    if (p->capacity > 0 && drows) {
-        hipLaunchKernelGGL(k_zero_unused, dim3(grid_for(a.rows, 4)), dim3(kThreads), 0, st, counts, a.rows, p->capacity,
-                           (size_t)p->d * elem_bytes(p), drows);
-        rc = launched();
-    }
-    return rc;
+    return p->dtype == MOE_DT_F32 ? pick_unsort_backward<float>(a, (hipStream_t)stream) : pick_unsort_backward<bf16_t>(a, (hipStream_t)stream);
 }
 
 size_t moe_backward_workspace_bytes(const moe_problem_t *p) {
