@@ -19,10 +19,18 @@ static unsigned grid_for(size_t n, size_t each) {
     return (unsigned)(g < (1u << 20) ? g : (1u << 20));
 }
 
+template <typename ET>
+static bool stream_rows(const UnsortArgs &a) {
+    return (size_t)a.rows * a.d * sizeof(ET) > kStreamBytes;
+}
 template <typename ET, int KB, int U, int G>
 static int launch_unsort(UnsortArgs &a, hipStream_t st) {
     a.parts = (a.d / Piece<ET>::N + G * U - 1) / (G * U);
-    hipLaunchKernelGGL((k_unsort<ET, KB, U, G>), dim3(grid_for((size_t)a.T * a.parts, kThreads / G)), dim3(kThreads), 0, st, a);
+    const dim3 grid(grid_for((size_t)a.T * a.parts, kThreads / G));
+    if (G == 64 && stream_rows<ET>(a))
+        hipLaunchKernelGGL((k_unsort<ET, KB, U, G, G == 64>), grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_unsort<ET, KB, U, G, false>), grid, dim3(kThreads), 0, st, a);
     return launched();
 }
 template <typename ET>
@@ -42,7 +50,11 @@ template <typename ET, int KB, int L>
 static int launch_unsort_backward(UnsortArgs &a, hipStream_t st) {
     a.token_groups = (int)grid_for(a.T, kThreads / L);
     const unsigned zero_groups = a.capacity > 0 && a.drows ? grid_for(a.rows, 16) : 0u;
-    hipLaunchKernelGGL((k_unsort_backward<ET, KB, L>), dim3(a.token_groups + zero_groups), dim3(kThreads), 0, st, a);
+    const dim3 grid(a.token_groups + zero_groups);
+    if (L >= 64 && stream_rows<ET>(a))
+        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, (L >= 64)>), grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, false>), grid, dim3(kThreads), 0, st, a);
     return launched();
 }
 template <typename ET, int L>

@@ -29,6 +29,20 @@ template <> struct Piece<bf16_t> {
     }
 };
 
+// Stores of results go past the caches (whoever reads them next finds them in memory; what the caches hold instead is the rows that are
+// read), and so do loads where a call reads more than they hold anyway.  us, loads and stores cached / stores past / both: 4096 x 8 rows
+// of 2048 (134 MB) 33.0 / 30.9 / 27.2, their gradient 60.5 / 59.1 / 55.3; 8192 x 16 of 320 (84 MB) 18.2 / 17.3 / 19.5, 16384 x 4 of 256
+// (34 MB) 9.5 / 9.5 / 11.4: from kStreamBytes on.
+constexpr size_t kStreamBytes = (size_t)96 << 20;
+template <typename T>
+__device__ __forceinline__ void store_past(T *p, T v) {
+    __builtin_nontemporal_store(v, p);
+}
+template <typename T>
+__device__ __forceinline__ T load_past(const T *p) {
+    return __builtin_nontemporal_load(p);
+}
+
 // A lane's value from the lane whose number differs in bit 0 (0xB1) or bit 1 (0x4E): no trip through LDS.
 template <int QUAD>
 __device__ __forceinline__ u32 quad_swap(u32 v) {

@@ -43,8 +43,8 @@ struct SlotRows {
 };
 
 // out[t] = addend[t] + sum_j w[t,j] sorted[inv_perm[t*k+j]]: G lanes take U pieces each of a token's row, KB rows in flight.  G < 64:
-// rows of at most G pieces, 64 / G tokens per wavefront.
-template <typename ET, int KB, int U, int G>
+// rows of at most G pieces, 64 / G tokens per wavefront.  STREAM: rows are read past the caches.
+template <typename ET, int KB, int U, int G, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_unsort(UnsortArgs a) {
     using P = Piece<ET>;
     static_assert(U == 1 || G == 64, "");
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void k_unsort(UnsortArgs a) {
             for (int j = 0; j < KB; ++j) {
                 const u32x4_t *row = (const u32x4_t *)a.sorted + (size_t)s.row[j] * pieces;
 #pragma unroll
-                for (int u = 0; u < U; ++u) v[j][u] = row[c[u]];
+                for (int u = 0; u < U; ++u) v[j][u] = STREAM ? load_past(row + c[u]) : row[c[u]];
             }
 #pragma unroll
             for (int j = 0; j < KB; ++j)
@@ -84,14 +84,14 @@ __global__ __launch_bounds__(kThreads) void k_unsort(UnsortArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (first + u * 64 < pieces) ((u32x4_t *)a.out)[(size_t)t * pieces + c[u]] = P::pack(acc[u]);
+            if (first + u * 64 < pieces) store_past((u32x4_t *)a.out + (size_t)t * pieces + c[u], P::pack(acc[u]));
     }
 }
 
 // drows[inv_perm[t*k+j]] = w[t,j] dout[t], dw[t,j] = <sorted[inv_perm[t*k+j]], dout[t]>: L lanes take a token (64 and fewer: of one
 // wavefront; more: wavefronts of a workgroup), KB rows at a time.  Every piece is read before it is written, by the same lane: drows may
 // be the rows.
-template <typename ET, int KB, int L>
+template <typename ET, int KB, int L, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_unsort_backward(UnsortArgs a) {
     using P = Piece<ET>;
     constexpr int G = L < 64 ? L : 64, WT = L / G, TOKENS = kThreads / L;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void k_unsort_backward(UnsortArgs a) {
         for (int r = ((int)blockIdx.x - a.token_groups) * 4 + wave; r < a.rows; r += groups * 4) {
             const int e = r / a.capacity;
             if (r - e * a.capacity < a.counts[e]) continue;
-            for (int c = threadIdx.x & 63; c < pieces; c += 64) ((u32x4_t *)a.drows)[(size_t)r * pieces + c] = u32x4_t{0, 0, 0, 0};
+            for (int c = threadIdx.x & 63; c < pieces; c += 64) store_past((u32x4_t *)a.drows + (size_t)r * pieces + c, u32x4_t{0, 0, 0, 0});
         }
         return;
     }
@@ -121,7 +121,10 @@ __global__ __launch_bounds__(kThreads) void k_unsort_backward(UnsortArgs a) {
                     u32x4_t v[KB];
                     if (a.dw) {
 #pragma unroll
-                        for (int j = 0; j < KB; ++j) v[j] = ((const u32x4_t *)a.sorted)[(size_t)s.row[j] * pieces + c];
+                        for (int j = 0; j < KB; ++j) {
+                            const u32x4_t *at = (const u32x4_t *)a.sorted + (size_t)s.row[j] * pieces + c;
+                            v[j] = STREAM ? load_past(at) : *at;
+                        }
                     }
                     P::unpack(gv, g);
 #pragma unroll
@@ -137,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_unsort_backward(UnsortArgs a) {
                                 float f[P::N];
 #pragma unroll
                                 for (int i = 0; i < P::N; ++i) f[i] = g[i] * s.w[j];
-                                ((u32x4_t *)a.drows)[(size_t)s.row[j] * pieces + c] = P::pack(f);
+                                store_past((u32x4_t *)a.drows + (size_t)s.row[j] * pieces + c, P::pack(f));
                             }
                         }
                 }
