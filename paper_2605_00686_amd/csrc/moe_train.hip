@@ -123,6 +123,36 @@ static int pick_gate_grad(const GateGradArgs &a, hipStream_t st) {
     return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, 2, 32, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, 2, 32, 2>>(a, st);
 }
 
+// Workgroups for all pieces of the rows.  (A grid has less than 2^32 threads; rows of so many pieces are more than the memory holds.)
+template <typename ET>
+static int swiglu_grid(const SwigluArgs &a, dim3 *grid) {
+    const size_t pieces = (size_t)a.rows * ((a.f + kScaleBlock - 1) / kScaleBlock * (kScaleBlock / Piece<ET>::N));
+    const size_t n = (pieces + kSwigluPieces * kThreads - 1) / (kSwigluPieces * kThreads);
+    if (n >= (1u << 24)) return MOE_ERR_UNSUPPORTED;
+    *grid = dim3((unsigned)n);
+    return MOE_OK;
+}
+template <typename ET>
+static int launch_swiglu(const SwigluArgs &a, hipStream_t st) {
+    dim3 grid;
+    if (const int rc = swiglu_grid<ET>(a, &grid)) return rc;
+    if ((size_t)a.rows * a.f * 2 * sizeof(ET) > kStreamBytes)
+        hipLaunchKernelGGL((k_swiglu<ET, true>), grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_swiglu<ET, false>), grid, dim3(kThreads), 0, st, a);
+    return launched();
+}
+template <typename ET>
+static int launch_swiglu_backward(const SwigluArgs &a, hipStream_t st) {
+    dim3 grid;
+    if (const int rc = swiglu_grid<ET>(a, &grid)) return rc;
+    if ((size_t)a.rows * a.f * (2 + sizeof(ET)) > kStreamBytes)
+        hipLaunchKernelGGL((k_swiglu_backward<ET, true>), grid, dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_swiglu_backward<ET, false>), grid, dim3(kThreads), 0, st, a);
+    return launched();
+}
+
 extern "C" {
 
 int moe_unsort(const moe_problem_t *p, const void *rows, const int32_t *inv_perm, const float *topk_w, const void *addend, void *out,
@@ -196,13 +226,7 @@ int moe_swiglu(const moe_problem_t *p, const void *g, const void *u, int64_t ld,
     SwigluArgs a = {};
     a.rows = rows_of(p); a.f = p->f; a.capacity = p->capacity; a.ld = ld;
     a.g = g; a.u = u; a.counts = counts; a.h = h; a.codes = codes; a.scales = scales;
-    const dim3 grid(grid_for((size_t)a.rows * ((p->f + kScaleBlock - 1) / kScaleBlock * 4), kThreads));
-    hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == MOE_DT_F32)
-        hipLaunchKernelGGL(k_swiglu<float>, grid, dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(k_swiglu<bf16_t>, grid, dim3(kThreads), 0, st, a);
-    return launched();
+    return p->dtype == MOE_DT_F32 ? launch_swiglu<float>(a, (hipStream_t)stream) : launch_swiglu<bf16_t>(a, (hipStream_t)stream);
 }
 
 int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *codes, const uint8_t *scales, const int32_t *counts,
@@ -216,13 +240,7 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
     a.rows = rows_of(p); a.f = p->f; a.capacity = p->capacity; a.ld = ld;
     a.dh = dh; a.counts = counts; a.dg = dg; a.du = du; a.h = h;
     a.codes = const_cast<uint8_t *>(codes); a.scales = const_cast<uint8_t *>(scales);
-    const dim3 grid(grid_for((size_t)a.rows * (p->f / kLaneValues), kThreads));
-    hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == MOE_DT_F32)
-        hipLaunchKernelGGL(k_swiglu_backward<float>, grid, dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(k_swiglu_backward<bf16_t>, grid, dim3(kThreads), 0, st, a);
-    return launched();
+    return p->dtype == MOE_DT_F32 ? launch_swiglu_backward<float>(a, (hipStream_t)stream) : launch_swiglu_backward<bf16_t>(a, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -43,10 +43,11 @@ __device__ __forceinline__ T load_past(const T *p) {
     return __builtin_nontemporal_load(p);
 }
 
-// A lane's value from the lane whose number differs in bit 0 (0xB1) or bit 1 (0x4E): no trip through LDS.
-template <int QUAD>
-__device__ __forceinline__ u32 quad_swap(u32 v) {
-    return (u32)__builtin_amdgcn_update_dpp(0, (int)v, QUAD, 0xf, 0xf, true);
+// A lane's value from another of its row of 16, without a trip through LDS: the lane whose number differs in bit 0 (0xB1) or bit 1
+// (0x4E), or the mirrored one of 8 (0x141).
+template <int CTRL>
+__device__ __forceinline__ u32 lane_swap(u32 v) {
+    return (u32)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
 
 __device__ __forceinline__ void report(int32_t *status, int code) {

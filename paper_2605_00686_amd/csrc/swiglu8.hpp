@@ -17,113 +17,172 @@ struct SwigluArgs {
 };
 
 constexpr int kScaleBlock = 32;  // values
-constexpr int kLaneValues = 8;   // consecutive values of a row that a lane holds: four lanes per block
 
-template <typename ET>
-__device__ __forceinline__ void load8(const void *p, size_t i, float *v) {
-    using P = Piece<ET>;
-#pragma unroll
-    for (int n = 0; n < 8 / P::N; ++n) P::unpack(*(const u32x4_t *)((const ET *)p + i + n * P::N), v + n * P::N);
+// A piece of a row (16 bytes; 8 values of bf16, 4 of fp32) is a lane's: a block is 4 or 8 neighbouring lanes.
+template <typename ET, bool STREAM>
+__device__ __forceinline__ u32x4_t load_piece(const void *p, size_t i) {
+    const u32x4_t *at = (const u32x4_t *)((const ET *)p + i);
+    return STREAM ? load_past(at) : *at;
 }
 template <typename ET>
-__device__ __forceinline__ void store8(void *p, size_t i, const float *v) {
-    using P = Piece<ET>;
-#pragma unroll
-    for (int n = 0; n < 8 / P::N; ++n) *(u32x4_t *)((ET *)p + i + n * P::N) = P::pack(v + n * P::N);
+__device__ __forceinline__ void store_piece(void *p, size_t i, const float *v) {
+    store_past((u32x4_t *)((ET *)p + i), Piece<ET>::pack(v));
 }
+// Codes of a piece: as many bytes as it has values
+template <int N> struct CodesOf;
+template <> struct CodesOf<8> { typedef u64 type; };
+template <> struct CodesOf<4> { typedef u32 type; };
 
-// Eight values as codes; `byte` is the block's scale.  The four lanes of a block call it together.
-__device__ __forceinline__ uint2 encode8(const float *v, u32 &byte) {
+// N values as codes; `byte` is the block's scale.  The lanes of a block call it together.
+template <int N>
+__device__ __forceinline__ typename CodesOf<N>::type encode(const float *v, u32 &byte) {
+    typedef __attribute__((ext_vector_type(2))) short s16x2_t;
     u32 most = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
         const u32 b = __float_as_uint(v[i]) & 0x7fffffffu;
         most = max(most, b < 0x7f800000u ? b : 0u);
     }
-    most = max(most, quad_swap<0xB1>(most));
-    most = max(most, quad_swap<0x4E>(most));
+    most = max(most, lane_swap<0xB1>(most));  // the neighbour,
+    most = max(most, lane_swap<0x4E>(most));  // the other pair of four,
+    if (N == 4) most = max(most, lane_swap<0x141>(most));  // the other four of eight
     // most = m 2^a with 1 <= m < 2 (448 = 1.75 * 2^8): 2^(a - 8), or twice that where m > 1.75
     byte = (u32)max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0), 0);
-    float s[8];
+    // the conversion takes the exponent of its scale alone, of an fp32 number's bits; it makes a NaN of what is not finite
+    const float scale = __uint_as_float(byte << 23);
+    u32 c[2] = {0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const bool finite = (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u;
-        s[i] = finite ? ldexpf(v[i], 127 - (int)byte) : __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < N / 4; ++i) {
+        s16x2_t w = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * i], v[4 * i + 1], scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * i + 2], v[4 * i + 3], scale, true);
+        c[i] = __builtin_bit_cast(u32, w);
     }
-    uint2 c = {0u, 0u};
-    c.x = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], (int)c.x, false);
-    c.x = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], (int)c.x, true);
-    c.y = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(s[4], s[5], (int)c.y, false);
-    c.y = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(s[6], s[7], (int)c.y, true);
-    return c;
+    return (typename CodesOf<N>::type)(N == 8 ? ((u64)c[1] << 32) | c[0] : (u64)c[0]);
 }
-__device__ __forceinline__ void decode8(uint2 c, u32 byte, float *v) {
-    const f32x2_t p[4] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, true),
-                          __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, true)};
+template <int N>
+__device__ __forceinline__ void decode(typename CodesOf<N>::type codes, u32 byte, float *v) {
+    const float scale = __uint_as_float(byte << 23);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = ldexpf(p[i >> 1][i & 1], (int)byte - 127);
+    for (int i = 0; i < N / 4; ++i) {
+        const u32 c = (u32)((u64)codes >> (32 * i));
+        const f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, true);
+        v[4 * i] = lo[0], v[4 * i + 1] = lo[1], v[4 * i + 2] = hi[0], v[4 * i + 3] = hi[1];
+    }
 }
 
 // 1 / (1 + exp(-g)); the exponential and the reciprocal of the hardware are within 2 units of fp32's last place for the g that
 // matter, far inside what the outputs are rounded to or compared at
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
-__device__ __forceinline__ bool row_used(const SwigluArgs &a, int row) {
-    if (a.capacity == 0) return true;
-    const int e = row / a.capacity;
-    return row - e * a.capacity < a.counts[e];
-}
-
-template <typename ET>
-__global__ __launch_bounds__(kThreads) void k_swiglu(SwigluArgs a) {
-    const int blocks = (a.f + kScaleBlock - 1) / kScaleBlock, per_row = blocks * 4;  // (lanes past the end of a row stay idle)
-    const size_t total = (size_t)a.rows * per_row, all = (total + kThreads - 1) / kThreads * kThreads;
-    for (size_t q = blockIdx.x * (size_t)kThreads + threadIdx.x; q < all; q += (size_t)gridDim.x * kThreads) {
-        const int row = (int)min(q / per_row, (size_t)a.rows - 1), piece = (int)(q - (size_t)row * per_row), c = piece * kLaneValues;
-        const bool mine = q < total && c < a.f;
-        float g[8] = {}, u[8] = {}, h[8];
-        if (mine && row_used(a, row)) {
-            load8<ET>(a.g, (size_t)row * a.ld + c, g);
-            load8<ET>(a.u, (size_t)row * a.ld + c, u);
-        }
+// A workgroup takes U * 256 pieces of the rows, a thread every 256th.  Rows are a whole number of blocks long here, so that the
+// lanes of a block are neighbours; pieces past a row's end stay idle.
+template <int N, int U>
+struct Pieces {
+    int row[U], c[U];  // c: first value
+    bool in[U];        // whether there is such a piece, in a row that is used
+    bool dead[U];      // ... in one that is not
+    __device__ __forceinline__ void find(const SwigluArgs &a) {
+        const int per_row = (a.f + kScaleBlock - 1) / kScaleBlock * (kScaleBlock / N);
+        const u64 q = blockIdx.x * (u64)(U * kThreads);
+        const u32 r0 = (u32)(q / (u32)per_row), x = (u32)(q - (u64)r0 * (u32)per_row) + threadIdx.x;
+        int r = (int)(r0 + x / (u32)per_row), p = (int)(x % (u32)per_row);
+        const int dr = kThreads / per_row, dp = kThreads - dr * per_row;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
-        if (mine && a.h) store8<ET>(a.h, (size_t)row * a.f + c, h);
+        for (int u = 0; u < U; ++u) {
+            row[u] = min(r, a.rows - 1), c[u] = min(p * N, a.f - N);
+            const bool there = r < a.rows && p * N < a.f;
+            bool used = true;
+            if (a.capacity) {
+                const int e = row[u] / a.capacity;
+                used = row[u] - e * a.capacity < a.counts[e];
+            }
+            in[u] = there && used, dead[u] = there && !used;
+            r += dr, p += dp;
+            if (p >= per_row) p -= per_row, ++r;
+        }
+    }
+};
+constexpr int kSwigluPieces = 2;  // per thread
+
+template <typename ET, bool STREAM>
+__global__ __launch_bounds__(kThreads) void k_swiglu(SwigluArgs a) {
+    constexpr int U = kSwigluPieces, N = Piece<ET>::N;
+    typedef typename CodesOf<N>::type Codes;
+    Pieces<N, U> at;
+    at.find(a);
+    u32x4_t gr[U], ur[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {  // (no load is conditional: the first row's where there is nothing to read)
+        const size_t i = at.in[u] ? (size_t)at.row[u] * a.ld + at.c[u] : 0;
+        gr[u] = load_piece<ET, STREAM>(a.g, i), ur[u] = load_piece<ET, STREAM>(a.u, i);
+    }
+    const int blocks = (a.f + kScaleBlock - 1) / kScaleBlock;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float g[N], v[N], h[N];
+        Piece<ET>::unpack(gr[u], g);
+        Piece<ET>::unpack(ur[u], v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            g[i] = at.in[u] ? g[i] : 0.f, v[i] = at.in[u] ? v[i] : 0.f;
+            h[i] = g[i] * sigmoid(g[i]) * v[i];
+        }
+        const bool mine = at.in[u] || at.dead[u];
+        const size_t row = at.row[u];
+        const int c = at.c[u];
+        if (mine && a.h) store_piece<ET>(a.h, row * a.f + c, h);
         if (!a.codes) continue;
         u32 sg, su;
-        const uint2 cg = encode8(g, sg), cu = encode8(u, su);
+        const Codes cg = encode<N>(g, sg), cu = encode<N>(v, su);
         if (!mine) continue;
-        *(uint2 *)(a.codes + (size_t)row * 2 * a.f + c) = cg;
-        *(uint2 *)(a.codes + ((size_t)row * 2 + 1) * a.f + c) = cu;
-        if ((piece & 3) == 0) {
-            a.scales[(size_t)row * 2 * blocks + piece / 4] = (uint8_t)sg;
-            a.scales[((size_t)row * 2 + 1) * blocks + piece / 4] = (uint8_t)su;
+        store_past((Codes *)(a.codes + row * 2 * a.f + c), cg);
+        store_past((Codes *)(a.codes + (row * 2 + 1) * a.f + c), cu);
+        if (c % kScaleBlock == 0) {
+            a.scales[row * 2 * blocks + c / kScaleBlock] = (uint8_t)sg;
+            a.scales[(row * 2 + 1) * blocks + c / kScaleBlock] = (uint8_t)su;
         }
     }
 }
 
-template <typename ET>
+template <typename ET, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_swiglu_backward(SwigluArgs a) {
-    const int blocks = (a.f + kScaleBlock - 1) / kScaleBlock, per_row = a.f / kLaneValues;
-    const size_t total = (size_t)a.rows * per_row;
-    for (size_t q = blockIdx.x * (size_t)kThreads + threadIdx.x; q < total; q += (size_t)gridDim.x * kThreads) {
-        const int row = (int)(q / per_row), piece = (int)(q - (size_t)row * per_row), c = piece * kLaneValues;
-        float g[8] = {}, u[8] = {}, dh[8] = {}, dg[8], du[8], h[8];
-        if (row_used(a, row)) {
-            load8<ET>(a.dh, (size_t)row * a.f + c, dh);
-            decode8(*(const uint2 *)(a.codes + (size_t)row * 2 * a.f + c), a.scales[(size_t)row * 2 * blocks + piece / 4], g);
-            decode8(*(const uint2 *)(a.codes + ((size_t)row * 2 + 1) * a.f + c), a.scales[((size_t)row * 2 + 1) * blocks + piece / 4], u);
-        }
+    constexpr int U = kSwigluPieces, N = Piece<ET>::N;
+    typedef typename CodesOf<N>::type Codes;
+    Pieces<N, U> at;
+    at.find(a);
+    const int blocks = (a.f + kScaleBlock - 1) / kScaleBlock;
+    u32x4_t dr[U];
+    Codes cg[U], cu[U];
+    u32 sg[U], su[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+    for (int u = 0; u < U; ++u) {
+        const size_t row = at.in[u] ? at.row[u] : 0;
+        const int c = at.in[u] ? at.c[u] : 0;
+        dr[u] = load_piece<ET, STREAM>(a.dh, row * a.f + c);
+        const Codes *pg = (const Codes *)(a.codes + row * 2 * a.f + c), *pu = (const Codes *)(a.codes + (row * 2 + 1) * a.f + c);
+        cg[u] = STREAM ? load_past(pg) : *pg, cu[u] = STREAM ? load_past(pu) : *pu;
+        sg[u] = a.scales[row * 2 * blocks + c / kScaleBlock], su[u] = a.scales[(row * 2 + 1) * blocks + c / kScaleBlock];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!at.in[u] && !at.dead[u]) continue;
+        float g[N], v[N], dh[N], dg[N], du[N], h[N];
+        Piece<ET>::unpack(dr[u], dh);
+        decode<N>(cg[u], sg[u], g);
+        decode<N>(cu[u], su[u], v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (at.dead[u]) g[i] = v[i] = dh[i] = 0.f;
             const float s = sigmoid(g[i]), silu = g[i] * s;
-            h[i] = silu * u[i];
+            h[i] = silu * v[i];
             du[i] = dh[i] * silu;
-            dg[i] = dh[i] * u[i] * s * (1.f + g[i] * (1.f - s));
+            dg[i] = dh[i] * v[i] * s * (1.f + g[i] * (1.f - s));
         }
-        store8<ET>(a.dg, (size_t)row * a.ld + c, dg);
-        store8<ET>(a.du, (size_t)row * a.ld + c, du);
-        if (a.h) store8<ET>(a.h, (size_t)row * a.f + c, h);
+        const size_t row = at.row[u];
+        store_piece<ET>(a.dg, row * a.ld + at.c[u], dg);
+        store_piece<ET>(a.du, row * a.ld + at.c[u], du);
+        if (a.h) store_piece<ET>(a.h, row * a.f + at.c[u], h);
     }
 }
 
