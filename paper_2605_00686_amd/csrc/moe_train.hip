@@ -93,7 +93,7 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     int each = units;
     for (int n = 1; n <= most && n <= units; ++n) {
         const int per = (units + n - 1) / n;
-        const double us = per * unit_us + n * part_us + (n > 1 ? 3.0 : 0.0);
+        const double us = per * unit_us + n * part_us + (n > 1 ? 3.0 + 0.05 * n : 0.0);
         if (n == 1 || us < best) best = us, each = per;
     }
     a->dw_tokens = each * kReduction;
@@ -110,7 +110,8 @@ static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
     hipLaunchKernelGGL(k_gate_grad<C>, dim3((a.dw_chunks + (a.dbias ? 1 : 0)) * a.dw_parts + a.dx_chunks * a.dx_parts), dim3(kGateGradThreads), smem, st, a);
     if (const int rc = launched()) return rc;
     if (a.dw_parts <= 1) return MOE_OK;
-    hipLaunchKernelGGL(k_gate_grad_join, dim3((unsigned)(((size_t)a.d * a.E / 4 + a.E + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a);
+    const size_t pieces = (size_t)a.d * a.E / 4 + (a.E + 3) / 4;
+    hipLaunchKernelGGL(k_gate_grad_join, dim3((unsigned)((pieces + 63) / 64)), dim3(kThreads), 0, st, a);
     return launched();
 }
 
