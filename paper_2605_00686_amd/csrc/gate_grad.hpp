@@ -198,7 +198,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     typedef __attribute__((ext_vector_type(16))) float f32x16_t;
     typedef __attribute__((ext_vector_type(8))) short s16x8_t;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int col0 = chunk * C::COLS, log2 = gate_lanes_log2(a.k);
+    const int col0 = chunk * C::COLS, log2 = C::PER == 1 ? 3 : gate_lanes_log2(a.k);  // (one pass: at most 8 choices)
     const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
     char *xs = smem + C::O_X;
     int *odd = (int *)(smem + C::O_ODD);  // first and last token whose x has a number here that is not finite
@@ -237,43 +237,40 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     u32 cut[C::PER][3];
 #pragma unroll
     for (int i = 0; i < C::PER; ++i) at[i] = old[i] = -1;
+    bool bad_id = false;
+    u32 odd_bits[C::NX];  // not 0: the piece has a number that is not finite
+    // (no branch on a number in here: the compiler deals these instructions out among a multiplication's)
     auto prepare = [&](int t0, u32x4_t(&row)[C::NX], GateSlots<C::PER> &slot) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < C::NX; ++m) {
-            u32x4_t v = row[m];
-            bool strange = false;
+            const u32x4_t v = row[m];
+            odd_bits[m] = 0u;
             if constexpr (sizeof(ET) == 2) {
-                u32 carry = 0u;  // of exponents that are all ones
 #pragma unroll
-                for (int q = 0; q < 4; ++q) carry |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                strange = carry != 0u;
-                if (strange) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
-                        if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
-                    }
-                }
+                for (int q = 0; q < 4; ++q) odd_bits[m] |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
                 piece[m][0] = uint2{v[0], v[1]}, piece[m][1] = uint2{v[2], v[3]};
             } else {
                 u32 b[4][3];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const bool fine = (v[q] & 0x7f800000u) != 0x7f800000u;
-                    strange |= !fine;
-                    cut3(fine ? __uint_as_float(v[q]) : 0.f, b[q]);
+                    odd_bits[m] |= ((v[q] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+                    cut3((v[q] & 0x7f800000u) != 0x7f800000u ? __uint_as_float(v[q]) : 0.f, b[q]);
                 }
 #pragma unroll
                 for (int n = 0; n < 3; ++n) piece[m][n] = uint2{(b[0][n] >> 16) | (b[1][n] & 0xffff0000u), (b[2][n] >> 16) | (b[3][n] & 0xffff0000u)};
             }
-            if (const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1); strange) atomicMin(&odd[0], t), atomicMax(&odd[1], t);
         }
+        const int j = tid & ((1 << log2) - 1), n_tok = min(C::KT, t_end - t0);
 #pragma unroll
-        for (int i = 0; i < C::PER; ++i) old[i] = at[i], at[i] = -1;
-        slot.finish(a, log2, min(C::KT, t_end - t0), [&](int i, int t, int, int e, float dl) {
-            at[i] = e < 0 ? -1 : e * C::DROW + t * 2;
+        for (int i = 0; i < C::PER; ++i) {
+            const int t = (tid + i * kGateGradThreads) >> log2, e = slot.e[i];
+            const float dl = slot.w[i] * (slot.dw[i] - gate_lanes_sum(slot.w[i] * slot.dw[i], log2));
+            const bool there = t < n_tok && j < a.k, fine = (u32)e < (u32)a.E;
+            bad_id |= there && !fine;
+            old[i] = at[i];
+            at[i] = there && fine ? e * C::DROW + t * 2 : -1;
             cut3(dl, cut[i]);
-        });
+        }
     };
     auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -305,9 +302,8 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                         for (int j = 0; j < C::CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - c][i], xv[c][j], acc[i][j], 0, 0, 0);
         }
     };
-    // The block at t0, whose numbers are prepared; `after` prepares the next one's.  The halves of the wavefronts, one of each on a
-    // SIMD, prepare before and after they multiply: one's vector instructions run beside the other's products.
-    auto block = [&](auto after) __attribute__((always_inline)) {
+    // The block at t0, whose numbers are prepared; `after` prepares the next one's, beside the products.
+    auto block = [&](int t0, auto after) __attribute__((always_inline)) {
         __syncthreads();  // (the block before is done with the LDS)
 #pragma unroll
         for (int i = 0; i < C::PER; ++i)
@@ -319,6 +315,18 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
             for (int m = 0; m < C::NX; ++m) {
                 char *to = xs + (x_tok + m * C::XSTEP) * C::XROW;
+                if (odd_bits[m]) {
+                    if constexpr (sizeof(ET) == 2) {
+                        u32 *v = (u32 *)piece[m];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
+                            if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
+                        }
+                    }
+                    const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1);
+                    atomicMin(&odd[0], t), atomicMax(&odd[1], t);
+                }
                 if constexpr (sizeof(ET) == 2)
                     *(u32x4_t *)(to + x_lane * 16) = u32x4_t{piece[m][0].x, piece[m][0].y, piece[m][1].x, piece[m][1].y};
                 else
@@ -334,9 +342,12 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                 for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)(cut[i][n] >> 16);
             }
         __syncthreads();
-        if (half == 0) after();
-        if (e0 < a.E) multiply();
-        if (half == 1) after();
+        if (e0 < a.E) {
+            multiply();
+            after();
+        } else {
+            after();
+        }
     };
     __syncthreads();  // (`odd` is set)
     for (int t0 = t_begin; t0 < t_end; t0 += GROUP * C::KT) {
@@ -353,11 +364,12 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
             if (t0 + i * C::KT >= t_end) break;
-            block([&]() __attribute__((always_inline)) {
+            block(t0 + i * C::KT, [&]() __attribute__((always_inline)) {
                 if (i + 1 < GROUP) prepare(t0 + (i + 1) * C::KT, x_now[(i + 1) % GROUP], slots_now[(i + 1) % GROUP]);
             });
         }
     }
+    if (bad_id) report(a.status, MOE_ERR_BAD_ROUTING);
     float *out = a.dw_parts == 1 ? a.dWg : a.parts + part * a.part_stride;
     // A lane has column lane % 32 of a block, and experts 8 q + 4 (lane / 32) .. + 3.  Through LDS, so that memory sees the chunk's rows of
     // dWg, which lie one behind the other, in one piece.
