@@ -24,7 +24,7 @@ constexpr int kGateGradSlots = 1024;  // dx: slots of a block of tokens, at most
 struct GateGradArgs {
     int T, d, E, k;
     int dx_chunks;             // dx: chunks of columns
-    int block;                 // dx: tokens of a block: block * k <= kGateGradSlots
+    int block;                 // dx: tokens of a block, of 8, 16 or 32 slots each (the power of two that holds k): kGateGradSlots in all
     int dx_parts, dx_blocks;   // dx: the tokens are cut into so many parts (0: no dx wanted) of so many blocks
     int dw_chunks;             // dWg: its chunks (0: not wanted)
     int dw_parts, dw_tokens;   // dWg and dbias: the tokens are cut into so many parts (0: neither wanted) of so many (a multiple of a reduction block)
@@ -39,7 +39,7 @@ struct GateGradArgs {
 };
 
 struct GateGradSlot {
-    int row;  // the slot's expert, E = none
+    int at;  // bytes from the first expert's columns of Wg in LDS to those of the slot's, or to zeros
     float dl;
 };
 
@@ -59,8 +59,6 @@ template <int PER>
 struct GateSlots {
     float w[PER], dw[PER];
     int e[PER];
-    // (whether the i-th pass lies past n tokens)
-    static __device__ __forceinline__ bool skip(int i, int log2, int n) { return i > 0 && ((i * kGateGradThreads) >> log2) >= n; }
     // tokens t0 .. t0 + n - 1
     __device__ __forceinline__ void load(const GateGradArgs &a, int log2, int t0, int n) {
         const int j = threadIdx.x & ((1 << log2) - 1);
@@ -79,7 +77,6 @@ struct GateSlots {
         const int j = threadIdx.x & ((1 << log2) - 1);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (skip(i, log2, n)) continue;
             const int t = (threadIdx.x + i * kGateGradThreads) >> log2;
             const float dl = w[i] * (dw[i] - gate_lanes_sum(w[i] * dw[i], log2));
             if (t >= n || j >= a.k) continue;
@@ -127,33 +124,35 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
     }
     if (wave == 0) *(u32 *)(wt + a.E * kChunkBytes + lane * 4) = 0u;
     const int group = threadIdx.x / 16, l16 = lane & 15, col = col0 + l16 * P::N;
+    const char *my_wt = wt + l16 * 16;
     for (int b = 0; b < a.dx_blocks; ++b) {
         const int t0 = (part * a.dx_blocks + b) * a.block, n = min(a.block, a.T - t0);
         if (n <= 0) break;
         __syncthreads();
-        slots.finish(a, log2, n, [&](int, int t, int j, int e, float dl) { l->slot[t * a.k + j] = e < 0 ? GateGradSlot{a.E, 0.f} : GateGradSlot{e, dl}; });
+        if ((int)(threadIdx.x & ((1 << log2) - 1)) >= a.k) {
+#pragma unroll
+            for (int i = 0; i < kGateGradSlots / kGateGradThreads; ++i) l->slot[threadIdx.x + i * kGateGradThreads] = GateGradSlot{a.E * kChunkBytes, 0.f};
+        }
+        slots.finish(a, log2, n, [&](int, int t, int j, int e, float dl) {
+            l->slot[(t << log2) + j] = e < 0 ? GateGradSlot{a.E * kChunkBytes, 0.f} : GateGradSlot{e * kChunkBytes, dl};
+        });
         __syncthreads();
         slots.load(a, log2, t0 + a.block, b + 1 < a.dx_blocks ? min(a.block, a.T - t0 - a.block) : 0);
         for (int t = group; t < n; t += kGateGradThreads / 16) {
             float acc[P::N] = {};
-            const GateGradSlot *mine = l->slot + t * a.k;
-            // (four rows at a time, the last ones made up with rows of zeros)
-            for (int j = 0; j < a.k; j += 4) {
-                GateGradSlot s[4];
-                u32x4_t v[4];
+            const GateGradSlot *mine = l->slot + (t << log2);
+            for (int j = 0; j < a.k; j += 4) {  // (four rows at a time, the last ones made up with rows of zeros)
+                u32x4_t s[2], v[4];
+                s[0] = *(const u32x4_t *)(mine + j), s[1] = *(const u32x4_t *)(mine + j + 2);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[i] = mine[min(j + i, a.k - 1)];
-                    if (j + i >= a.k) s[i] = GateGradSlot{a.E, 0.f};
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = *(const u32x4_t *)(wt + s[i].row * kChunkBytes + l16 * 16);
+                for (int i = 0; i < 4; ++i) v[i] = *(const u32x4_t *)(my_wt + s[i / 2][i % 2 * 2]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float f[P::N];
                     P::unpack(v[i], f);
+                    const float dl = __uint_as_float(s[i / 2][i % 2 * 2 + 1]);
 #pragma unroll
-                    for (int q = 0; q < P::N; ++q) acc[q] = fmaf(s[i].dl, f[q], acc[q]);
+                    for (int q = 0; q < P::N; ++q) acc[q] = fmaf(dl, f[q], acc[q]);
                 }
             }
             if (col < a.d) *(u32x4_t *)((ET *)a.dx + (size_t)(t0 + t) * a.d + col) = P::pack(acc);
