@@ -155,7 +155,7 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
                     for (int q = 0; q < P::N; ++q) acc[q] = fmaf(dl, f[q], acc[q]);
                 }
             }
-            if (col < a.d) *(u32x4_t *)((ET *)a.dx + (size_t)(t0 + t) * a.d + col) = P::pack(acc);
+            if (col < a.d) store_past((u32x4_t *)((ET *)a.dx + (size_t)(t0 + t) * a.d + col), P::pack(acc));
         }
     }
 }
