@@ -18,7 +18,8 @@ namespace moe {
 
 constexpr int kGateGradThreads = 512, kGateGradWaves = kGateGradThreads / 64;
 constexpr int kChunkBytes = 256;      // dx: of a row, and of a column of Wg
-constexpr int kGateDwCols = 64;       // dWg: columns of a task
+constexpr int kGateDwCols = 64;       // dWg: columns of a task ...
+constexpr int kGateDwExperts = 128;   // ... and experts, at most
 constexpr int kGateGradSlots = 1024;  // dx: slots of a block of tokens, at most
 
 struct GateGradArgs {
@@ -26,7 +27,8 @@ struct GateGradArgs {
     int dx_chunks;             // dx: chunks of columns
     int block;                 // dx: tokens of a block, of 8, 16 or 32 slots each (the power of two that holds k): kGateGradSlots in all
     int dx_parts, dx_blocks;   // dx: the tokens are cut into so many parts (0: no dx wanted) of so many blocks
-    int dw_chunks;             // dWg: its chunks (0: not wanted)
+    int dw_chunks;             // dWg: chunks of columns (0: not wanted)
+    int dw_groups, dw_experts; // ... groups of so many experts (a multiple of 4)
     int dw_parts, dw_tokens;   // dWg and dbias: the tokens are cut into so many parts (0: neither wanted) of so many (a multiple of a reduction block)
     const void *x, *Wg;
     const int32_t *idx;
@@ -168,13 +170,14 @@ __device__ __forceinline__ void cut3(float v, u32 *b) {
     b[2] = __float_as_uint(r - __uint_as_float(b[1]));
 }
 
-// Shape of a dWg task: KT tokens per reduction block, of which either half of the 8 wavefronts multiplies one half; a wavefront has EB
-// blocks of 32 experts and all columns.  (What a step reads from LDS bounds it: three pieces of dl per block of 32 experts, so every
+// Shape of a dWg task: KT tokens per reduction block, of which either half of the 8 wavefronts multiplies one half; a wavefront has
+// 32 of up to 128 experts and all columns.  (What a step reads from LDS bounds it: three pieces of dl per block of 32 experts, so every
 // wavefront uses them on 64 columns.)
-template <typename ET_, int EB_, int KT_, int PER_>
+template <typename ET_, int KT_, int PER_>
 struct GateDwShape {
     using ET = ET_;
-    static constexpr int EB = EB_, KT = KT_, WE = 4, COLS = kGateDwCols, CB = COLS / 32, EPAD = EB * WE * 32;
+    static constexpr int KT = KT_, WE = 4, COLS = kGateDwCols, CB = COLS / 32, EPAD = kGateDwExperts;
+    static_assert(WE * 32 == EPAD, "");
     static constexpr int XP = sizeof(ET) == 4 ? 3 : 1;  // bf16 numbers that make up one of x
     // Rows of LDS.  dl, [3][EPAD][KT] bf16: 16 bytes behind each row, so that 16 lanes' pieces of 16 bytes meet no bank twice; x,
     // [XP][KT][COLS] bf16: rows 16 banks apart modulo 64, for the transposing read of 4 rows x 64 bytes.
@@ -182,16 +185,15 @@ struct GateDwShape {
     static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
     static constexpr int O_X = 3 * DPLANE, TURN = COLS * (EPAD + 4) * 4;
     static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + 16;
-    static constexpr int WAVES = XP * EB > 3 ? 2 : 4;  // on a SIMD; the largest takes more registers than two workgroups of a CU have
     static constexpr int GROUP = PER_ == 1 ? 2 : 1;  // blocks whose numbers are loaded together
     static constexpr int PER = PER_;                   // passes over the slots of a reduction block
     static constexpr int LANES = COLS / Piece<ET>::N;  // of a row of x, a piece each
     static constexpr int NX = (KT * LANES + kGateGradThreads - 1) / kGateGradThreads, XSTEP = kGateGradThreads / LANES;  // pieces per thread, tokens apart
 };
-// dWg[columns of a chunk, :] over the tokens of a part.  For a reduction block of tokens dl
+// dWg[columns of a chunk, experts of a group] over the tokens of a part.  For a reduction block of tokens dl
 // lies dense in LDS, by expert: its slots are written there, multiplied, and cleared again.
 template <class C>
-__device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, int chunk, int part) {
+__device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, int chunk, int group, int part) {
     using ET = typename C::ET;
     using P = Piece<ET>;
     typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -199,6 +201,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int col0 = chunk * C::COLS, log2 = C::PER == 1 ? 3 : gate_lanes_log2(a.k);  // (one pass: at most 8 choices)
     const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
+    const int e_first = group * a.dw_experts, n_e = min(a.E - e_first, a.dw_experts);
     char *xs = smem + C::O_X;
     int *odd = (int *)(smem + C::O_ODD);  // first and last token whose x has a number here that is not finite
     // Loads run a group of blocks ahead, whole groups at a time: a block's tokens are few, and a CU may have one workgroup
@@ -222,14 +225,12 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     load_group(t_begin);
     for (int i = tid * 16; i < C::O_X; i += kGateGradThreads * 16) *(u32x4_t *)(smem + i) = u32x4_t{0, 0, 0, 0};
     if (tid == 0) odd[0] = 0x7fffffff, odd[1] = -1;
-    const int half = wave / C::WE, e0 = wave % C::WE * C::EB * 32;
-    f32x16_t acc[C::EB][C::CB];
+    const int half = wave / C::WE, e0 = wave % C::WE * 32;
+    f32x16_t acc[C::CB];
 #pragma unroll
-    for (int i = 0; i < C::EB; ++i)
+    for (int j = 0; j < C::CB; ++j)
 #pragma unroll
-        for (int j = 0; j < C::CB; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+        for (int q = 0; q < 16; ++q) acc[j][q] = 0.f;
     // A block's numbers on their way from memory to LDS: this thread's piece of x as bf16 numbers, and its slots
     uint2 piece[C::NX][sizeof(ET) == 2 ? 2 : 3];
     int at[C::PER], old[C::PER];  // where its slots lie in dl, -1 = it has none; and those of the block before
@@ -262,12 +263,12 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
         const int j = tid & ((1 << log2) - 1), n_tok = min(C::KT, t_end - t0);
 #pragma unroll
         for (int i = 0; i < C::PER; ++i) {
-            const int t = (tid + i * kGateGradThreads) >> log2, e = slot.e[i];
+            const int t = (tid + i * kGateGradThreads) >> log2, e = slot.e[i] - e_first;
             const float dl = slot.w[i] * (slot.dw[i] - gate_lanes_sum(slot.w[i] * slot.dw[i], log2));
-            const bool there = t < n_tok && j < a.k, fine = (u32)e < (u32)a.E;
-            bad_id |= there && !fine;
+            const bool there = t < n_tok && j < a.k;
+            bad_id |= there && (u32)slot.e[i] >= (u32)a.E;
             old[i] = at[i];
-            at[i] = there && fine ? e * C::DROW + t * 2 : -1;
+            at[i] = there && (u32)e < (u32)n_e ? e * C::DROW + t * 2 : -1;
             cut3(dl, cut[i]);
         }
     };
@@ -275,12 +276,10 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
         for (int n = 0; n < C::KT / 32; ++n) {
             const int kk = half * (C::KT / 32) + n;
-            bf16x8_t dl[3][C::EB], xv[C::XP][C::CB];
+            bf16x8_t dl[3], xv[C::XP][C::CB];
 #pragma unroll
             for (int c = 2; c >= 0; --c)
-#pragma unroll
-                for (int i = 0; i < C::EB; ++i)
-                    dl[c][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(smem + c * C::DPLANE + (e0 + i * 32 + (lane & 31)) * C::DROW + (kk * 16 + 8 * (lane >> 5)) * 2));
+                dl[c] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(smem + c * C::DPLANE + (e0 + (lane & 31)) * C::DROW + (kk * 16 + 8 * (lane >> 5)) * 2));
 #pragma unroll
             for (int c = 0; c < C::XP; ++c)
 #pragma unroll
@@ -296,9 +295,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
                 for (int c = 0; c < C::XP && c <= order; ++c)
 #pragma unroll
-                    for (int i = 0; i < C::EB; ++i)
-#pragma unroll
-                        for (int j = 0; j < C::CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - c][i], xv[c][j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < C::CB; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dl[order - c], xv[c][j], acc[j], 0, 0, 0);
         }
     };
     // The block at t0, whose numbers are prepared; `after` prepares the next one's, beside the products.
@@ -341,7 +338,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                 for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)(cut[i][n] >> 16);
             }
         __syncthreads();
-        if (e0 < a.E) {
+        if (e0 < n_e) {
             multiply();
             after();
         } else {
@@ -374,35 +371,34 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     // dWg, which lie one behind the other, in one piece.
     const int stride = C::EPAD + 4;
     float *turn = (float *)smem;
-    auto mine = [&](int i, int j, int q) {
-        const f32x16_t &v = acc[i][j];
+    auto mine = [&](int j, int q) {
+        const f32x16_t &v = acc[j];
         return f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
     };
     for (int h = 1; h >= 0; --h) {  // one half's sums, then the other's added to them
         __syncthreads();
         if (half != h) continue;
 #pragma unroll
-        for (int i = 0; i < C::EB; ++i)
+        for (int j = 0; j < C::CB; ++j)
 #pragma unroll
-            for (int j = 0; j < C::CB; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    f32x4_t &to = *(f32x4_t *)(turn + (j * 32 + (lane & 31)) * stride + e0 + i * 32 + 8 * q + 4 * (lane >> 5));
-                    to = h ? mine(i, j, q) : to + mine(i, j, q);
-                }
+            for (int q = 0; q < 4; ++q) {
+                f32x4_t &to = *(f32x4_t *)(turn + (j * 32 + (lane & 31)) * stride + e0 + 8 * q + 4 * (lane >> 5));
+                to = h ? mine(j, q) : to + mine(j, q);
+            }
     }
     __syncthreads();
-    const int n_out = min(C::COLS, a.d - col0) * a.E, step = a.E % 4 == 0 ? 4 : 1;
-    float *to = out + (size_t)col0 * a.E;
-    int c = tid * step / a.E, e = tid * step - c * a.E;
-    const int dc = kGateGradThreads * step / a.E, de = kGateGradThreads * step - dc * a.E;
+    // (of all experts a chunk's rows are one piece of memory)
+    const int step = a.E % 4 == 0 ? 4 : 1, n_out = min(C::COLS, a.d - col0) * n_e;
+    float *to = out + (size_t)col0 * a.E + e_first;
+    int c = tid * step / n_e, e = tid * step - c * n_e;
+    const int dc = kGateGradThreads * step / n_e, de = kGateGradThreads * step - dc * n_e;
     for (int i = tid * step; i < n_out; i += kGateGradThreads * step) {
         if (step == 4)
-            *(f32x4_t *)(to + i) = *(const f32x4_t *)(turn + c * stride + e);
+            *(f32x4_t *)(to + (size_t)c * a.E + e) = *(const f32x4_t *)(turn + c * stride + e);
         else
-            to[i] = turn[c * stride + e];
+            to[(size_t)c * a.E + e] = turn[c * stride + e];
         c += dc, e += de;
-        if (e >= a.E) e -= a.E, ++c;
+        if (e >= n_e) e -= n_e, ++c;
     }
     sync_stores();
     if (odd[1] < 0) return;
@@ -416,7 +412,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
         float mean = 0.f;
         for (int j = 0; j < a.k; ++j) mean += a.w[s + j] * a.dw[s + j];
         for (int j = 0; j < a.k; ++j)
-            if ((u32)a.idx[s + j] < (u32)a.E) out[(size_t)col * a.E + a.idx[s + j]] += v * (a.w[s + j] * (a.dw[s + j] - mean));
+            if ((u32)(a.idx[s + j] - e_first) < (u32)n_e) out[(size_t)col * a.E + a.idx[s + j]] += v * (a.w[s + j] * (a.dw[s + j] - mean));
     }
 }
 
@@ -443,12 +439,12 @@ __device__ __forceinline__ void gate_bias_task(const GateGradArgs &a, char *smem
 }
 
 template <class C>
-__global__ __launch_bounds__(kGateGradThreads, C::WAVES) void k_gate_grad(GateGradArgs a) {
+__global__ __launch_bounds__(kGateGradThreads, 4) void k_gate_grad(GateGradArgs a) {
     extern __shared__ __align__(16) char smem[];
     // dWg's tasks, dbias's, then dx's
-    const int n_w = a.dw_chunks * a.dw_parts, n_b = n_w + (a.dbias ? a.dw_parts : 0), task = blockIdx.x;
+    const int n_c = a.dw_chunks * a.dw_groups, n_w = n_c * a.dw_parts, n_b = n_w + (a.dbias ? a.dw_parts : 0), task = blockIdx.x;
     if (task < n_w)
-        gate_dw_task<C>(a, smem, task % a.dw_chunks, task / a.dw_chunks);
+        gate_dw_task<C>(a, smem, task % n_c / a.dw_groups, task % a.dw_groups, task / n_c);
     else if (task < n_b)
         gate_bias_task(a, smem, task - n_w);
     else

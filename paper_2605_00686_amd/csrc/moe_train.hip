@@ -81,14 +81,16 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int blocks = (p->T + a->block - 1) / a->block, dx_want = parts_of(512, a->dx_chunks);
     a->dx_blocks = (blocks + dx_want - 1) / dx_want;
     a->dx_parts = (blocks + a->dx_blocks - 1) / a->dx_blocks;
-    // Parts of dWg: a reduction block takes a task 1 us (64 tokens, or 32 beyond 128 experts), a part's sums 0.6 us per MB to write and read
-    // again, and the launch that adds them up 3 us.  At most one task per CU: two share it, and the sums of twice as many parts cost more
-    // than that gains.  us, 4096 x 8 of 128 of 2048, parts 4 / 8 / 16: 24.3 / 20.5 / 25.3; 2048 x 8 of 256 of 7168, 1 / 2 / 4: 63.1 / 40.4
-    // / 36.4, but with dx beside it 64.1 / 42.9 / 46.3; 512 x 8 of 128 of 2048, 1 / 8: @@ / 12.7.
+    // Parts of dWg's tokens: 64 of them take a task 0.85 us (1.75 in fp32), a part's sums 0.8 us per MB to write and read again, and the
+    // launch that adds them up 3 us.  At most one task per CU, so that dx's, which share the CUs, do not wait.  us, with dx, by parts:
+    // 4096 x 8 of 128 of 2048 4 / 8 / 16: 23.0 / 22.8 / 24.2, 1024 tokens 1 / 4 / 16: 18.3 / 11.9 / 20.0; 2048 x 8 of 256 of 7168 1 / 2 / 4:
+    // 34.5 / 41.2 / 44.8; 16384 x 4 of 32 of 64 16 / 64 / 256: 19.0 / 10.2 / 14.4.
     constexpr int kReduction = 64;  // tokens, a multiple of every shape's
     a->dw_chunks = (p->d + kGateDwCols - 1) / kGateDwCols;
-    const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(256, a->dw_chunks);
-    const double unit_us = p->E > 128 || p->dtype == MOE_DT_F32 ? 2.0 : 1.0, part_us = 0.6e-6 * 4.0 * p->d * p->E;
+    a->dw_groups = (p->E + kGateDwExperts - 1) / kGateDwExperts;
+    a->dw_experts = ((p->E + a->dw_groups - 1) / a->dw_groups + 3) / 4 * 4;
+    const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(256, a->dw_chunks * a->dw_groups);
+    const double unit_us = p->dtype == MOE_DT_F32 ? 1.75 : 0.85, part_us = 0.8e-6 * 4.0 * p->d * p->E;
     double best = 0.0;
     int each = units;
     for (int n = 1; n <= most && n <= units; ++n) {
@@ -107,7 +109,7 @@ static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
     const size_t dw = a.dw_chunks ? (size_t)C::LDS : 0, db = a.dbias ? (size_t)kGateGradThreads / 8 * a.E * 4 : 0;
     const size_t smem = dx > dw ? (dx > db ? dx : db) : (dw > db ? dw : db);
     if (const int rc = allow_lds((const void *)k_gate_grad<C>, smem)) return rc;
-    hipLaunchKernelGGL(k_gate_grad<C>, dim3((a.dw_chunks + (a.dbias ? 1 : 0)) * a.dw_parts + a.dx_chunks * a.dx_parts), dim3(kGateGradThreads), smem, st, a);
+    hipLaunchKernelGGL(k_gate_grad<C>, dim3((a.dw_chunks * a.dw_groups + (a.dbias ? 1 : 0)) * a.dw_parts + a.dx_chunks * a.dx_parts), dim3(kGateGradThreads), smem, st, a);
     if (const int rc = launched()) return rc;
     if (a.dw_parts <= 1) return MOE_OK;
     const size_t pieces = (size_t)a.d * a.E / 4 + (a.E + 3) / 4;
@@ -115,13 +117,10 @@ static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
     return launched();
 }
 
-// KT tokens per reduction block up to 128 experts, 32 beyond (the LDS that dl takes there); one pass over their slots for up to 8
-// choices, else as many as 32 choices take.
+// One pass over a reduction block's slots for up to 8 choices, else as many as 32 choices take.
 template <typename ET, int KT>
 static int pick_gate_grad(const GateGradArgs &a, hipStream_t st) {
-    constexpr int MANY = KT * 32 / kGateGradThreads;
-    if (a.E <= 128) return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, 1, KT, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, 1, KT, MANY>>(a, st);
-    return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, 2, 32, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, 2, 32, 2>>(a, st);
+    return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, KT, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, KT, KT * 32 / kGateGradThreads>>(a, st);
 }
 
 // Workgroups for all pieces of the rows.  (A grid has less than 2^32 threads; rows of so many pieces are more than the memory holds.)
