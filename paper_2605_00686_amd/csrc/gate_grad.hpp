@@ -170,14 +170,15 @@ __device__ __forceinline__ void cut3(float v, u32 *b) {
     b[2] = __float_as_uint(r - __uint_as_float(b[1]));
 }
 
-// Shape of a dWg task: KT tokens per reduction block, of which either half of the 8 wavefronts multiplies one half; a wavefront has
-// 32 of up to 128 experts and all columns.  (What a step reads from LDS bounds it: three pieces of dl per block of 32 experts, so every
-// wavefront uses them on 64 columns.)
-template <typename ET_, int KT_, int PER_>
+// Shape of a dWg task: KT tokens per reduction block; a wavefront has 32 of up to 32 WE experts and all columns, and the 8 / WE
+// wavefronts that have the same multiply a share of the block each.  FEW: at most 8 choices.  (What a step reads from LDS bounds it:
+// three pieces of dl per block of 32 experts, so every wavefront uses them on 64 columns.)
+template <typename ET_, int WE_, int KT_, bool FEW_>
 struct GateDwShape {
     using ET = ET_;
-    static constexpr int KT = KT_, WE = 4, COLS = kGateDwCols, CB = COLS / 32, EPAD = kGateDwExperts;
-    static_assert(WE * 32 == EPAD, "");
+    static constexpr int WE = WE_, KT = KT_, SHARES = kGateGradWaves / WE, STEPS = KT / 16 / SHARES, COLS = kGateDwCols, CB = COLS / 32, EPAD = WE * 32;
+    static_assert(STEPS * SHARES * 16 == KT && EPAD <= kGateDwExperts, "");
+    static constexpr bool FEW = FEW_;
     static constexpr int XP = sizeof(ET) == 4 ? 3 : 1;  // bf16 numbers that make up one of x
     // Rows of LDS.  dl, [3][EPAD][KT] bf16: 16 bytes behind each row, so that 16 lanes' pieces of 16 bytes meet no bank twice; x,
     // [XP][KT][COLS] bf16: rows 16 banks apart modulo 64, for the transposing read of 4 rows x 64 bytes.
@@ -185,11 +186,12 @@ struct GateDwShape {
     static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
     static constexpr int O_X = 3 * DPLANE, TURN = COLS * (EPAD + 4) * 4;
     static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + 16;
-    static constexpr int GROUP = PER_ == 1 ? 2 : 1;  // blocks whose numbers are loaded together
-    static constexpr int PER = PER_;                   // passes over the slots of a reduction block
+    static constexpr int SLOT_LANES = KT * (FEW ? 8 : 32), PER = SLOT_LANES < kGateGradThreads ? 1 : SLOT_LANES / kGateGradThreads;  // passes over a block's slots
+    static constexpr int GROUP = FEW ? 2 : 1;          // blocks whose numbers are loaded together
     static constexpr int LANES = COLS / Piece<ET>::N;  // of a row of x, a piece each
     static constexpr int NX = (KT * LANES + kGateGradThreads - 1) / kGateGradThreads, XSTEP = kGateGradThreads / LANES;  // pieces per thread, tokens apart
 };
+
 // dWg[columns of a chunk, experts of a group] over the tokens of a part.  For a reduction block of tokens dl
 // lies dense in LDS, by expert: its slots are written there, multiplied, and cleared again.
 template <class C>
@@ -199,7 +201,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     typedef __attribute__((ext_vector_type(16))) float f32x16_t;
     typedef __attribute__((ext_vector_type(8))) short s16x8_t;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int col0 = chunk * C::COLS, log2 = C::PER == 1 ? 3 : gate_lanes_log2(a.k);  // (one pass: at most 8 choices)
+    const int col0 = chunk * C::COLS, log2 = C::FEW ? 3 : gate_lanes_log2(a.k);
     const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
     const int e_first = group * a.dw_experts, n_e = min(a.E - e_first, a.dw_experts);
     char *xs = smem + C::O_X;
@@ -225,7 +227,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     load_group(t_begin);
     for (int i = tid * 16; i < C::O_X; i += kGateGradThreads * 16) *(u32x4_t *)(smem + i) = u32x4_t{0, 0, 0, 0};
     if (tid == 0) odd[0] = 0x7fffffff, odd[1] = -1;
-    const int half = wave / C::WE, e0 = wave % C::WE * 32;
+    const int share = wave / C::WE, e0 = wave % C::WE * 32;
     f32x16_t acc[C::CB];
 #pragma unroll
     for (int j = 0; j < C::CB; ++j)
@@ -274,8 +276,8 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     };
     auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < C::KT / 32; ++n) {
-            const int kk = half * (C::KT / 32) + n;
+        for (int n = 0; n < C::STEPS; ++n) {
+            const int kk = share * C::STEPS + n;
             bf16x8_t dl[3], xv[C::XP][C::CB];
 #pragma unroll
             for (int c = 2; c >= 0; --c)
@@ -375,15 +377,15 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
         const f32x16_t &v = acc[j];
         return f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
     };
-    for (int h = 1; h >= 0; --h) {  // one half's sums, then the other's added to them
+    for (int h = C::SHARES - 1; h >= 0; --h) {  // one share's sums, then the others' added to them
         __syncthreads();
-        if (half != h) continue;
+        if (share != h) continue;
 #pragma unroll
         for (int j = 0; j < C::CB; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 f32x4_t &to = *(f32x4_t *)(turn + (j * 32 + (lane & 31)) * stride + e0 + 8 * q + 4 * (lane >> 5));
-                to = h ? mine(j, q) : to + mine(j, q);
+                to = h == C::SHARES - 1 ? mine(j, q) : to + mine(j, q);
             }
     }
     __syncthreads();

@@ -81,7 +81,7 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int blocks = (p->T + a->block - 1) / a->block, dx_want = parts_of(512, a->dx_chunks);
     a->dx_blocks = (blocks + dx_want - 1) / dx_want;
     a->dx_parts = (blocks + a->dx_blocks - 1) / a->dx_blocks;
-    // Parts of dWg's tokens: 64 of them take a task 0.85 us (1.75 in fp32), a part's sums 0.8 us per MB to write and read again, and the
+    // Parts of dWg's tokens: 64 of them take a task 0.85 us (1.3 to 1.75 in fp32), a part's sums 0.8 us per MB to write and read again, and the
     // launch that adds them up 3 us.  At most one task per CU, so that dx's, which share the CUs, do not wait.  us, with dx, by parts:
     // 4096 x 8 of 128 of 2048 4 / 8 / 16: 23.0 / 22.8 / 24.2, 1024 tokens 1 / 4 / 16: 18.3 / 11.9 / 20.0; 2048 x 8 of 256 of 7168 1 / 2 / 4:
     // 34.5 / 41.2 / 44.8; 16384 x 4 of 32 of 64 16 / 64 / 256: 19.0 / 10.2 / 14.4.
@@ -90,7 +90,7 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     a->dw_groups = (p->E + kGateDwExperts - 1) / kGateDwExperts;
     a->dw_experts = ((p->E + a->dw_groups - 1) / a->dw_groups + 3) / 4 * 4;
     const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(256, a->dw_chunks * a->dw_groups);
-    const double unit_us = p->dtype == MOE_DT_F32 ? 1.75 : 0.85, part_us = 0.8e-6 * 4.0 * p->d * p->E;
+    const double unit_us = p->dtype == MOE_DT_F32 ? (p->E <= 64 ? 1.3 : 1.75) : 0.85, part_us = 0.8e-6 * 4.0 * p->d * p->E;
     double best = 0.0;
     int each = units;
     for (int n = 1; n <= most && n <= units; ++n) {
@@ -117,10 +117,16 @@ static int launch_gate_grad(const GateGradArgs &a, hipStream_t st) {
     return launched();
 }
 
-// One pass over a reduction block's slots for up to 8 choices, else as many as 32 choices take.
-template <typename ET, int KT>
+template <typename ET, int WE, int KT>
 static int pick_gate_grad(const GateGradArgs &a, hipStream_t st) {
-    return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, KT, 1>>(a, st) : launch_gate_grad<GateDwShape<ET, KT, KT * 32 / kGateGradThreads>>(a, st);
+    return a.k <= 8 ? launch_gate_grad<GateDwShape<ET, WE, KT, true>>(a, st) : launch_gate_grad<GateDwShape<ET, WE, KT, false>>(a, st);
+}
+// Up to 64 experts take shapes of their own: half as much of dl's LDS, and for fp32 twice as many tokens per block.  us, with the shapes of
+// 128 / their own: bf16 16384 x 4 of 64 of 512 16.9 / 15.5; fp32 9683 x 3 of 3 of 720 21.2 / 18.5, 256 x 2 of 8 of 512 10.6 / 8.5.
+template <typename ET>
+static int pick_gate_grad(const GateGradArgs &a, hipStream_t st) {
+    if (a.E <= 64) return pick_gate_grad<ET, 2, 64>(a, st);
+    return pick_gate_grad<ET, 4, sizeof(ET) == 2 ? 64 : 32>(a, st);
 }
 
 // Workgroups for all pieces of the rows.  (A grid has less than 2^32 threads; rows of so many pieces are more than the memory holds.)
@@ -206,7 +212,7 @@ int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, co
     if (!dx) a.dx_parts = 0;
     a.parts = (float *)workspace;
     hipStream_t st = (hipStream_t)stream;
-    return p->dtype == MOE_DT_F32 ? pick_gate_grad<float, 32>(a, st) : pick_gate_grad<bf16_t, 64>(a, st);
+    return p->dtype == MOE_DT_F32 ? pick_gate_grad<float>(a, st) : pick_gate_grad<bf16_t>(a, st);
 }
 
 static int check_swiglu(const moe_problem_t *p, int64_t ld, const int32_t *counts, const void *codes, const void *scales) {
