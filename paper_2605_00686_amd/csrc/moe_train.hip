@@ -81,15 +81,16 @@ static void gate_grad_plan(const moe_problem_t *p, GateGradArgs *a) {
     const int blocks = (p->T + a->block - 1) / a->block, dx_want = parts_of(512, a->dx_chunks);
     a->dx_blocks = (blocks + dx_want - 1) / dx_want;
     a->dx_parts = (blocks + a->dx_blocks - 1) / a->dx_blocks;
-    // Parts of dWg's tokens: 64 of them take a task 0.85 us (1.3 to 1.75 in fp32), a part's sums 0.8 us per MB to write and read again, and the
-    // launch that adds them up 3 us.  At most one task per CU, so that dx's, which share the CUs, do not wait.  us, with dx, by parts:
-    // 4096 x 8 of 128 of 2048 4 / 8 / 16: 23.0 / 22.8 / 24.2, 1024 tokens 1 / 4 / 16: 18.3 / 11.9 / 20.0; 2048 x 8 of 256 of 7168 1 / 2 / 4:
-    // 34.5 / 41.2 / 44.8; 16384 x 4 of 32 of 64 16 / 64 / 256: 19.0 / 10.2 / 14.4.
+    // Parts of dWg's tokens: 64 of them take a task 0.85 us (1.3 to 1.75 in fp32), a part's sums 0.8 us per MB to write and read again, and
+    // the launch that adds them up 3 us.  At most three tasks for four CUs: dx's, which share the CUs, would wait for them.  us, with dx, by
+    // parts: 4096 x 8 of 128 of 2048 4 / 6 / 8 / 16: 23.0 / 20.7 / 22.8 / 24.1, 1024 tokens 1 / 4 / 16: 18.2 / 11.9 / 19.9; 2048 x 8 of 256
+    // of 7168 1 / 2 / 4: 35.3 / 40.9 / 44.8; 16384 x 4 of 32 of 64 16 / 64 / 256: 17.9 / 9.8 / 13.4; 9683 x 3 of 3 of 720 (fp32) 16 / 21:
+    // 19.8 / 18.5.  (By the problem alone, whichever gradients are wanted: their bits are the same alone and together.)
     constexpr int kReduction = 64;  // tokens, a multiple of every shape's
     a->dw_chunks = (p->d + kGateDwCols - 1) / kGateDwCols;
     a->dw_groups = (p->E + kGateDwExperts - 1) / kGateDwExperts;
     a->dw_experts = ((p->E + a->dw_groups - 1) / a->dw_groups + 3) / 4 * 4;
-    const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(256, a->dw_chunks * a->dw_groups);
+    const int units = (p->T + kReduction - 1) / kReduction, most = parts_of(192, a->dw_chunks * a->dw_groups);
     const double unit_us = p->dtype == MOE_DT_F32 ? (p->E <= 64 ? 1.3 : 1.75) : 0.85, part_us = 0.8e-6 * 4.0 * p->d * p->E;
     double best = 0.0;
     int each = units;
