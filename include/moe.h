@@ -279,8 +279,8 @@ int moe_combine(const moe_problem_t *p, const void *staging, const uint32_t *fla
  * nothing, and nothing of it is read.  Any other number outside the rows does the same and is reported as
  * MOE_ERR_BAD_ROUTING in status_dev (int32 on the device, may be NULL, written only on failure).  No two slots may
  * have the same row.  `counts` is needed where rows are padded and may be NULL where they are not; unused rows are
- * never read, and come out as zeros.  Sums are fp32; tensors of `dtype` and codes start on 16 bytes
- * (else MOE_ERR_INVALID_ARG).  Outputs may not overlap inputs except where it says so.  The calls keep nothing
+ * never read, and come out as zeros.  Sums are fp32; tensors of `dtype`, codes and dWg start on 16
+ * bytes (else MOE_ERR_INVALID_ARG).  Outputs may not overlap inputs except where it says so.  The calls keep nothing
  * and clear nothing: the same inputs give the same bits.
  */
 
@@ -310,7 +310,7 @@ size_t moe_backward_workspace_bytes(const moe_problem_t *p);
  * (dtopk_w[t,j] - sum_i topk_w[t,i] dtopk_w[t,i]): dx[t] = sum_j dl[t,j] Wg[:,topk_idx[t,j]], one rounding;
  * dWg[:,e] and dgate_bias[e] = the sums of dl x[t] and of dl over the slots that chose e.
  *   dx [T,d] dtype, dWg [d,E] fp32, dgate_bias [E] fp32 out; each may be NULL.  Wg is needed for dx, x for dWg.
- *   An id outside [0,E) is MOE_ERR_BAD_ROUTING in status_dev; its slot has no gradient (its share of the sum over i
+ *   The k ids of a token are distinct.  An id outside [0,E) is MOE_ERR_BAD_ROUTING in status_dev; its slot has no gradient (its share of the sum over i
  *   counts).  workspace: moe_backward_workspace_bytes() bytes, 256-byte aligned; needed for dWg and dgate_bias.
  */
 int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx,
@@ -323,6 +323,7 @@ int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, co
  *   g, u: [rows, f] dtype, `ld` elements from one row to the next in both (>= f, whole multiples of 16 bytes): two
  *   tensors of their own, or the halves of one [rows, 2f].  h [rows, f] out, may be NULL.
  *   codes [rows][2][f] bytes, scales [rows][2][ceil(f/32)] bytes out (g first, then u); both or none may be NULL.
+ *   More than 2^24 * 512 pieces of 16 bytes are MOE_ERR_UNSUPPORTED.
  *   Every 32 values of a row (the last 16, where f is an odd multiple of 16) share a power of two: scales holds its
  *   exponent + 127 (E8M0), the least that brings the block's largest finite value to 448 or less, at least 0; codes
  *   holds value / 2^exponent as e4m3 (OCP), rounded to nearest even.  A value that is not finite becomes the code of

@@ -1,7 +1,15 @@
 // SwiGLU with its inputs kept in 8 bits, and its gradient from them.
 //
 // Blocks of 32 values of a row share a power of two: e4m3 has 4 bits of precision wherever its exponent reaches (2^-6 to 448), so
-// a block's scale only has to bring its values there, and a power of two does that without a rounding of its own.
+// a block's scale only has to bring its values there, and a power of two does that without a rounding of its own.  A value is
+// then off by at most 2^-4 of itself (or 2^-10 of the scale), which is what halving bf16's bytes costs the gradient; sums are not
+// concerned.  The largest of a block is found among the lanes that hold it, the conversions are the hardware's scaled ones.
+//
+// Bound by memory: 2 f elements read, f written and 2 f (1 + 1/32) bytes kept per row; backward f elements and the kept bytes read, 3 f
+// elements written.  A lane holds 16 bytes of an input (wider pieces leave half lines per store: fp32 4096 x 1040, gradient, 16.4 us
+// with 8 values per lane, 13.2 with 4), two pieces per thread.  Measured, MI355X, bf16, inputs that change from call to call (the
+// runtime's copy moves 4.7 TB/s there): 32768 rows of 768 36.4 us = 5.6 TB/s, 8192 of 2048 22.3 us, gradient 25.9; 32768 of 14336 635 us = 6.0
+// TB/s, gradient 808 us = 5.9.
 #pragma once
 #include "pieces.hpp"
 
