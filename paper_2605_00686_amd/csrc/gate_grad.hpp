@@ -196,7 +196,8 @@ struct GateDwShape {
     static constexpr int SLOT_LANES = KT * (FEW ? 8 : 32), PER = SLOT_LANES < kGateGradThreads ? 1 : SLOT_LANES / kGateGradThreads;  // passes over a block's slots
     static constexpr int GROUP = FEW ? 2 : 1;          // blocks whose numbers are loaded together
     static constexpr int LANES = COLS / Piece<ET>::N;  // of a row of x, a piece each
-    static constexpr int NX = (KT * LANES + kGateGradThreads - 1) / kGateGradThreads, XSTEP = kGateGradThreads / LANES;  // pieces per thread, tokens apart
+    static constexpr int NX = KT * LANES / kGateGradThreads, XSTEP = kGateGradThreads / LANES;  // pieces per thread, tokens apart
+    static_assert(NX * kGateGradThreads == KT * LANES, "whole pieces per thread");
 };
 
 // dWg[columns of a chunk, experts of a group] over the tokens of a part.  For a reduction block of tokens dl
@@ -217,8 +218,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     constexpr int GROUP = C::GROUP;
     u32x4_t rows[GROUP][C::NX];
     GateSlots<C::PER> slots[GROUP];
-    const int x_tok = tid / C::LANES % C::KT, x_lane = tid % C::LANES;
-    const bool x_mine = tid < C::KT * C::LANES;
+    const int x_tok = tid / C::LANES, x_lane = tid % C::LANES;
     const ET *x = (const ET *)a.x + min(col0 + x_lane * P::N, a.d - P::N);
     // (no load is conditional: the number of loads in flight is then known at every wait)
     auto load_x = [&](u32x4_t(&v)[C::NX], int t0) __attribute__((always_inline)) {
@@ -316,28 +316,26 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
                 for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + old[i]) = 0;
             }
-        if (x_mine) {
 #pragma unroll
-            for (int m = 0; m < C::NX; ++m) {
-                char *to = xs + (x_tok + m * C::XSTEP) * C::XROW;
-                if (odd_bits[m]) {
-                    if constexpr (sizeof(ET) == 2) {
-                        u32 *v = (u32 *)piece[m];
+        for (int m = 0; m < C::NX; ++m) {
+            char *to = xs + (x_tok + m * C::XSTEP) * C::XROW;
+            if (odd_bits[m]) {
+                if constexpr (sizeof(ET) == 2) {
+                    u32 *v = (u32 *)piece[m];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
-                            if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
-                        }
+                    for (int q = 0; q < 4; ++q) {
+                        if ((v[q] & 0x7f80u) == 0x7f80u) v[q] &= 0xffff0000u;
+                        if ((v[q] & 0x7f800000u) == 0x7f800000u) v[q] &= 0xffffu;
                     }
-                    const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1);
-                    atomicMin(&odd[0], t), atomicMax(&odd[1], t);
                 }
-                if constexpr (sizeof(ET) == 2)
-                    *(u32x4_t *)(to + x_lane * 16) = u32x4_t{piece[m][0].x, piece[m][0].y, piece[m][1].x, piece[m][1].y};
-                else
-#pragma unroll
-                    for (int n = 0; n < 3; ++n) *(uint2 *)(to + n * C::XPLANE + x_lane * 8) = piece[m][n];
+                const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1);
+                atomicMin(&odd[0], t), atomicMax(&odd[1], t);
             }
+            if constexpr (sizeof(ET) == 2)
+                *(u32x4_t *)(to + x_lane * 16) = u32x4_t{piece[m][0].x, piece[m][0].y, piece[m][1].x, piece[m][1].y};
+            else
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *(uint2 *)(to + n * C::XPLANE + x_lane * 8) = piece[m][n];
         }
         __syncthreads();
 #pragma unroll
