@@ -191,7 +191,7 @@ struct GateDwShape {
     // [XP][KT][COLS] bf16: rows 16 banks apart modulo 64, for the transposing read of 4 rows x 64 bytes.
     static constexpr int DROW = KT * 2 + 16, XROW = COLS * 2 + 64;
     static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
-    static constexpr int O_X = 3 * DPLANE, TURN = COLS * (EPAD + 4) * 4;
+    static constexpr int O_X = 3 * DPLANE, TROW = EPAD + 4, TURN = SHARES * COLS * TROW * 4;
     static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + 16;
     static constexpr int SLOT_LANES = KT * (FEW ? 8 : 32), PER = SLOT_LANES < kGateGradThreads ? 1 : SLOT_LANES / kGateGradThreads;  // passes over a block's slots
     static constexpr int GROUP = FEW ? 2 : 1;          // blocks whose numbers are loaded together
@@ -376,23 +376,15 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     float *out = a.dw_parts == 1 ? a.dWg : a.parts + part * a.part_stride;
     // A lane has column lane % 32 of a block, and experts 8 q + 4 (lane / 32) .. + 3.  Through LDS, so that memory sees the chunk's rows of
     // dWg, which lie one behind the other, in one piece.
-    const int stride = C::EPAD + 4;
-    float *turn = (float *)smem;
-    auto mine = [&](int j, int q) {
-        const f32x16_t &v = acc[j];
-        return f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-    };
-    for (int h = C::SHARES - 1; h >= 0; --h) {  // one share's sums, then the others' added to them
-        __syncthreads();
-        if (share != h) continue;
+    float *turn = (float *)smem;  // [SHARES][COLS][TROW]
+    __syncthreads();
 #pragma unroll
-        for (int j = 0; j < C::CB; ++j)
+    for (int j = 0; j < C::CB; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                f32x4_t &to = *(f32x4_t *)(turn + (j * 32 + (lane & 31)) * stride + e0 + 8 * q + 4 * (lane >> 5));
-                to = h == C::SHARES - 1 ? mine(j, q) : to + mine(j, q);
-            }
-    }
+        for (int q = 0; q < 4; ++q) {
+            const f32x16_t &v = acc[j];
+            *(f32x4_t *)(turn + (share * C::COLS + j * 32 + (lane & 31)) * C::TROW + e0 + 8 * q + 4 * (lane >> 5)) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        }
     __syncthreads();
     // (of all experts a chunk's rows are one piece of memory)
     const int step = a.E % 4 == 0 ? 4 : 1, n_out = min(C::COLS, a.d - col0) * n_e;
@@ -400,10 +392,18 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     int c = tid * step / n_e, e = tid * step - c * n_e;
     const int dc = kGateGradThreads * step / n_e, de = kGateGradThreads * step - dc * n_e;
     for (int i = tid * step; i < n_out; i += kGateGradThreads * step) {
-        if (step == 4)
-            *(f32x4_t *)(to + (size_t)c * a.E + e) = *(const f32x4_t *)(turn + c * stride + e);
-        else
-            to[(size_t)c * a.E + e] = turn[c * stride + e];
+        const float *from = turn + c * C::TROW + e;
+        if (step == 4) {
+            f32x4_t sum = *(const f32x4_t *)from;
+#pragma unroll
+            for (int h = 1; h < C::SHARES; ++h) sum += *(const f32x4_t *)(from + h * C::COLS * C::TROW);
+            *(f32x4_t *)(to + (size_t)c * a.E + e) = sum;
+        } else {
+            float sum = *from;
+#pragma unroll
+            for (int h = 1; h < C::SHARES; ++h) sum += from[h * C::COLS * C::TROW];
+            to[(size_t)c * a.E + e] = sum;
+        }
         c += dc, e += de;
         if (e >= n_e) e -= n_e, ++c;
     }
