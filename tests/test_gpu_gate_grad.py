@@ -222,3 +222,16 @@ def test_not_finite_inputs_reach_the_chosen_experts_and_tokens_only(T, d, E, k, 
     (_, _), (ref, bound), (ref_b, bound_b) = expected(idx, w, dw, clean, torch.zeros_like(Wg), dt)
     assert bool(((dWg.double() - ref).abs() <= bound)[~bad].all())
     assert bool(((db.double() - ref_b).abs() <= bound_b).all())
+
+
+# several parts of the tokens together with two groups of experts, whose number is odd or a multiple of 4 and not of 8, and chunks of columns cut short
+@pytest.mark.parametrize("case", [(2500, 144, 131, 3, "f32"), (2100, 192, 129, 9, "bf16"), (3001, 64, 244, 2, "bf16"), (1900, 448, 65, 5, "bf16"),
+                                  (1700, 80, 68, 12, "f32"), (5000, 64, 64, 1, "bf16"), (1111, 704, 256, 17, "f32")],
+                         ids=lambda c: "T%d_d%d_E%d_k%d_%s" % c)
+def test_parts_and_groups(case):
+    print(f"case parts and groups {case}", flush=True)
+    B, p, gen, dt, idx, w, dw, x, Wg = make(*case)
+    got = call(B, p, x, Wg, idx, w, dw)
+    check(got, expected(idx, w, dw, x, Wg, dt))
+    assert torch.equal(call(B, p, x, Wg, idx, w, dw, "w")[1], got[1])
+    assert torch.equal(call(B, p, x, Wg, idx, w, dw, "b")[2], got[2])
