@@ -19,6 +19,10 @@ static unsigned grid_for(size_t n, size_t each) {
     return (unsigned)(g < (1u << 20) ? g : (1u << 20));
 }
 
+// Few tokens: below the first number a token's slots are several workgroups (the gradient of 17 x 16 rows of 3968 9.7 -> 6.9 us, 500 x 32 of 512
+// 15.3 -> 8.8; 1000 x 16 of 2048 24.1 -> 24.9), up to the second a long row a workgroup of 1024 threads (fp32 8 x 8 rows of 2368 8.5 -> 7.5;
+// bf16 64 x 8 of 7168 9.0 -> 9.1, 500 x 8 22.3 -> 25.8).
+constexpr int kFewTokens = 512, kVeryFewTokens = 32;
 template <typename ET>
 static bool stream_rows(const UnsortArgs &a) {
     return (size_t)a.rows * a.d * sizeof(ET) > kStreamBytes;
@@ -50,20 +54,22 @@ static int pick_unsort(UnsortArgs &a, hipStream_t st) {
 
 template <typename ET, int KB, int L>
 static int launch_unsort_backward(UnsortArgs &a, hipStream_t st) {
-    a.token_groups = (int)grid_for(a.T, kThreads / L);
-    const unsigned zero_groups = a.capacity > 0 && a.drows ? grid_for(a.rows, 16) : 0u;
+    constexpr int NT = unsort_backward_threads(L);
+    a.batches = a.T < kFewTokens ? (a.k + KB - 1) / KB : 1;
+    a.token_groups = (int)grid_for(a.T, NT / L) * a.batches;
+    const unsigned zero_groups = a.capacity > 0 && a.drows ? grid_for(a.rows, NT / 16) : 0u;
     const dim3 grid(a.token_groups + zero_groups);
     if (L >= 64 && stream_rows<ET>(a))
-        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, (L >= 64)>), grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, (L >= 64)>), grid, dim3(NT), 0, st, a);
     else
-        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, false>), grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((k_unsort_backward<ET, KB, L, false>), grid, dim3(NT), 0, st, a);
     return launched();
 }
 template <typename ET, int L>
 static int pick_unsort_backward(UnsortArgs &a, hipStream_t st) {
     return a.k <= 2 ? launch_unsort_backward<ET, 2, L>(a, st) : a.k <= 4 ? launch_unsort_backward<ET, 4, L>(a, st) : launch_unsort_backward<ET, 8, L>(a, st);
 }
-// Lanes per token by the row's length, up to a workgroup: 4096 x 8 rows of 2048 with 64 / 128 / 256 lanes 71 / 65 / 59 us.
+// Lanes per token by the row's length: 4096 x 8 rows of 2048 with 64 / 128 / 256 lanes 71 / 65 / 59 us.
 template <typename ET>
 static int pick_unsort_backward(UnsortArgs &a, hipStream_t st) {
     const int pieces = a.d / Piece<ET>::N;
@@ -71,7 +77,8 @@ static int pick_unsort_backward(UnsortArgs &a, hipStream_t st) {
     if (pieces <= 16) return pick_unsort_backward<ET, 16>(a, st);
     if (pieces <= 32) return pick_unsort_backward<ET, 32>(a, st);
     if (pieces <= 64) return pick_unsort_backward<ET, 64>(a, st);
-    return pieces <= 128 ? pick_unsort_backward<ET, 128>(a, st) : pick_unsort_backward<ET, 256>(a, st);
+    if (pieces <= 128) return pick_unsort_backward<ET, 128>(a, st);
+    return pieces <= 256 || a.T > kVeryFewTokens ? pick_unsort_backward<ET, 256>(a, st) : pick_unsort_backward<ET, 1024>(a, st);
 }
 
 // How the gate's gradient is cut.

@@ -13,7 +13,7 @@ namespace moe {
 struct UnsortArgs {
     int T, d, k, rows, capacity;  // rows of the sorted order; capacity 0 = ragged
     int parts;                    // forward: groups of lanes per token
-    int token_groups;             // backward: workgroups that take tokens; those behind them clear unused rows
+    int token_groups, batches;    // backward: workgroups that take tokens, `batches` the slots of one; those behind them clear unused rows
     const void *sorted, *addend, *dout;
     const int32_t *inv_perm, *counts;
     const float *w;  // NULL = ones
@@ -93,27 +93,30 @@ __global__ __launch_bounds__(kThreads) void k_unsort(UnsortArgs a) {
     }
 }
 
+constexpr int unsort_backward_threads(int lanes) { return lanes > kThreads ? lanes : kThreads; }
+
 // drows[inv_perm[t*k+j]] = w[t,j] dout[t], dw[t,j] = <sorted[inv_perm[t*k+j]], dout[t]>: L lanes take a token (64 and fewer: of one
 // wavefront; more: wavefronts of a workgroup), KB rows at a time.  Every piece is read before it is written, by the same lane: drows may
 // be the rows.
 template <typename ET, int KB, int L, bool STREAM>
-__global__ __launch_bounds__(kThreads) void k_unsort_backward(UnsortArgs a) {
+__global__ __launch_bounds__(unsort_backward_threads(L)) void k_unsort_backward(UnsortArgs a) {
     using P = Piece<ET>;
-    constexpr int G = L < 64 ? L : 64, WT = L / G, TOKENS = kThreads / L;
-    __shared__ float sums[4][KB];
+    constexpr int NT = unsort_backward_threads(L), G = L < 64 ? L : 64, WT = L / G, TOKENS = NT / L;
+    __shared__ float sums[NT / 64][KB];
     const int lane = threadIdx.x & (G - 1), wave = uniform(threadIdx.x >> 6), pieces = a.d / P::N;
     if ((int)blockIdx.x >= a.token_groups) {  // padded layout: the rows behind an expert's used ones become zero
         const int groups = gridDim.x - a.token_groups;
-        for (int r = ((int)blockIdx.x - a.token_groups) * 4 + wave; r < a.rows; r += groups * 4) {
+        for (int r = ((int)blockIdx.x - a.token_groups) * (NT / 64) + wave; r < a.rows; r += groups * (NT / 64)) {
             const int e = r / a.capacity;
             if (r - e * a.capacity < a.counts[e]) continue;
             for (int c = threadIdx.x & 63; c < pieces; c += 64) store_past((u32x4_t *)a.drows + (size_t)r * pieces + c, u32x4_t{0, 0, 0, 0});
         }
         return;
     }
-    for (int t0 = blockIdx.x * TOKENS; t0 < a.T; t0 += a.token_groups * TOKENS) {
+    const int step = a.token_groups / a.batches * TOKENS;
+    for (int t0 = (int)blockIdx.x / a.batches * TOKENS; t0 < a.T; t0 += step) {
         const int t = t0 + (L < 64 ? (int)threadIdx.x / L : wave / WT);
-        for (int j0 = 0; j0 < a.k; j0 += KB) {
+        for (int j0 = (int)blockIdx.x % a.batches * KB; j0 < a.k; j0 += a.batches * KB) {
             SlotRows<KB> s;
             s.load(a, min(t, a.T - 1), j0);
             float sum[KB] = {};

@@ -231,3 +231,12 @@ def test_other_stream_and_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, (out, drows, dw)))
         both()
         torch.cuda.synchronize()
+
+
+# where the gradient's workgroups change: slots of a token apart below 512 tokens, workgroups of 1024 threads for long rows up to 32 tokens
+@pytest.mark.parametrize("case", [(32, 2368, 9, 9, 0, "f32"), (33, 2368, 9, 9, 0, "f32"), (32, 2112, 40, 17, 12, "bf16"), (7, 16448, 33, 32, 0, "bf16"),
+                                  (511, 1024, 24, 24, 0, "bf16"), (512, 1024, 24, 24, 0, "bf16"), (511, 64, 20, 20, 400, "bf16"), (31, 8192, 8, 1, 5, "f32")],
+                         ids=lambda c: "T%d_d%d_E%d_k%d_C%d_%s" % c)
+def test_few_tokens(case):
+    test_unsort_backward(case, True)
+    test_unsort_backward(case, False)
