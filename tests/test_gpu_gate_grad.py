@@ -235,3 +235,12 @@ def test_parts_and_groups(case):
     check(got, expected(idx, w, dw, x, Wg, dt))
     assert torch.equal(call(B, p, x, Wg, idx, w, dw, "w")[1], got[1])
     assert torch.equal(call(B, p, x, Wg, idx, w, dw, "b")[2], got[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_expert(dtype):
+    # a weight of exactly one has no gradient; any other is treated as given
+    B, p, gen, dt, idx, w, dw, x, Wg = make(130, 128, 1, 1, dtype)
+    assert all(float(g.abs().max()) == 0.0 for g in call(B, p, x, Wg, idx, w, dw))
+    w = torch.rand(130, 1, generator=gen)
+    check(call(B, p, x, Wg, idx, w, dw), expected(idx, w, dw, x, Wg, dt))
