@@ -8,9 +8,9 @@
 //
 // dWg = x^T dl is a product of the matrix cores, with the zeros: one instruction takes 16 tokens x 32 columns x 32 experts.  Listing a
 // block's slots by expert and adding up their rows on the vector ALU took 30 us where this takes 17 (the listing is a chain of five
-// barriers, and the rows of an expert few).  fp32 numbers are cut into three bf16 numbers that add up to them exactly (8 bits each,
-// truncated), and products below 2^-24 of the largest are left out, so sums are as good as fp32's; a number of x that is not finite is
-// left out of the dense product, where it would make a NaN of every expert's sum, and added for its token's experts alone.
+// barriers, and the rows of an expert few).  fp32 numbers are cut into three bf16 numbers that add up to them exactly, and the products
+// of the smaller ones are left out: a product is then off by less than 2^-24 of itself, a rounding of fp32, and towards neither side
+// (see cut3).  A number of x that is not finite is left out of the dense product, where it would make a NaN of every expert's sum, and added for its token's experts alone.
 // What bounds it: a task's chain per 64 tokens of LDS writes, three barriers and 12 matrix instructions per wavefront, 0.8 us of
 // which the matrix cores are busy 0.3, with one task per CU because every part of the tokens costs its sums (d E fp32) a trip to
 // memory and back.
@@ -169,12 +169,27 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
     }
 }
 
-// A finite fp32 number as three bf16 numbers in the upper halves, 8 bits of it each (an infinity becomes one and two NaNs).
-__device__ __forceinline__ void cut3(float v, u32 *b) {
-    b[0] = __float_as_uint(v) & 0xffff0000u;
-    const float r = v - __uint_as_float(b[0]);
-    b[1] = __float_as_uint(r) & 0xffff0000u;
-    b[2] = __float_as_uint(r - __uint_as_float(b[1]));
+// Two finite fp32 numbers as three bf16 numbers each that add up to them exactly, in the halves of b[0], b[1], b[2] (of a number that is
+// not finite one is a NaN at least).  Each is the bf16 number nearest to what those before it leave: with 2^e <= |v| < 2^(e+1) the second is
+// 2^(e-8) at most and the third, of the 7 bits that are left, 2^(e-17), so the two products of order 3 come to 2^-24 of the whole at
+// most, of either sign.  (Cut off instead of rounded they came to 2^-21, always towards zero: 0.7 * 2^-24 of a sum on average, however
+// many terms it has.)  Only the first may be rounded past bf16's largest: it stops there.
+__device__ __forceinline__ void cut3(float lo, float hi, u32 *b) {
+    constexpr float kLargest = 0x1.fep127f;
+    b[0] = pack_bf16x2(__builtin_amdgcn_fmed3f(lo, -kLargest, kLargest), __builtin_amdgcn_fmed3f(hi, -kLargest, kLargest));
+#pragma unroll
+    for (int n = 1; n < 3; ++n) {
+        lo -= __uint_as_float(b[n - 1] << 16), hi -= __uint_as_float(b[n - 1] & 0xffff0000u);
+        b[n] = pack_bf16x2(lo, hi);
+    }
+}
+// One such number cut off every 8 bits, in the lower halves: where no product is left out (x of bf16) that is exact too, and a shorter
+// chain (rounded: 2048 x 8 of 256 of 7168 33.4 -> 34.1 us, 16384 x 2 of 8 of 4096 71.6 -> 73.4).
+__device__ __forceinline__ void cut3_off(float v, u32 *b) {
+    b[0] = __float_as_uint(v) >> 16;
+    const float r = v - __uint_as_float(b[0] << 16);
+    b[1] = __float_as_uint(r) >> 16;
+    b[2] = __float_as_uint(r - __uint_as_float(b[1] << 16)) >> 16;
 }
 
 // Shape of a dWg task: KT tokens per reduction block; a wavefront has 32 of up to 32 WE experts and all columns, and the 8 / WE
@@ -259,14 +274,16 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                 for (int q = 0; q < 4; ++q) odd_bits[m] |= ((v[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
                 piece[m][0] = uint2{v[0], v[1]}, piece[m][1] = uint2{v[2], v[3]};
             } else {
-                u32 b[4][3];
+                float f[4];
+                u32 b[2][3];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     odd_bits[m] |= ((v[q] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
-                    cut3((v[q] & 0x7f800000u) != 0x7f800000u ? __uint_as_float(v[q]) : 0.f, b[q]);
+                    f[q] = (v[q] & 0x7f800000u) != 0x7f800000u ? __uint_as_float(v[q]) : 0.f;
                 }
+                cut3(f[0], f[1], b[0]), cut3(f[2], f[3], b[1]);
 #pragma unroll
-                for (int n = 0; n < 3; ++n) piece[m][n] = uint2{(b[0][n] >> 16) | (b[1][n] & 0xffff0000u), (b[2][n] >> 16) | (b[3][n] & 0xffff0000u)};
+                for (int n = 0; n < 3; ++n) piece[m][n] = uint2{b[0][n], b[1][n]};
             }
         }
         const int j = tid & ((1 << log2) - 1), n_tok = min(C::KT, t_end - t0);
@@ -278,7 +295,10 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
             bad_id |= there && (u32)slot.e[i] >= (u32)a.E;
             old[i] = at[i];
             at[i] = there && (u32)e < (u32)n_e ? e * C::DROW + t * 2 : -1;
-            cut3(dl, cut[i]);
+            if constexpr (C::XP == 1)
+                cut3_off(dl, cut[i]);
+            else
+                cut3(dl, 0.f, cut[i]);
         }
     };
     auto multiply = [&]() __attribute__((always_inline)) {
@@ -298,7 +318,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                     const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(p + 4 * C::XROW));
                     xv[c][j] = __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
-            // the smallest products first; those below 2^-24 of the largest are left out
+            // the smallest products first; those of order 3 and 4 are left out (cut3)
 #pragma unroll
             for (int order = 2; order >= 0; --order)
 #pragma unroll
@@ -342,7 +362,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
         for (int i = 0; i < C::PER; ++i)
             if (at[i] >= 0) {
 #pragma unroll
-                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)(cut[i][n] >> 16);
+                for (int n = 0; n < 3; ++n) *(unsigned short *)(smem + n * C::DPLANE + at[i]) = (unsigned short)cut[i][n];
             }
         __syncthreads();
         if (e0 < n_e) {
