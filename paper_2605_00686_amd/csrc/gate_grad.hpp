@@ -10,7 +10,8 @@
 // block's slots by expert and adding up their rows on the vector ALU took 30 us where this takes 17 (the listing is a chain of five
 // barriers, and the rows of an expert few).  fp32 numbers are cut into three bf16 numbers that add up to them exactly, and the products
 // of the smaller ones are left out: a product is then off by less than 2^-24 of itself, a rounding of fp32, and towards neither side
-// (see cut3).  A number of x that is not finite is left out of the dense product, where it would make a NaN of every expert's sum, and added for its token's experts alone.
+// (see cut3).  A number of x that is not finite is left out of the dense product, where it would make a NaN of every expert's sum, and
+// added for its token's experts alone; an infinite dl makes a NaN of its own expert's sums there, which are then taken again.
 // What bounds it: a task's chain per 64 tokens of LDS writes, three barriers and 12 matrix instructions per wavefront, 0.8 us of
 // which the matrix cores are busy 0.3, with one task per CU because every part of the tokens costs its sums (d E fp32) a trip to
 // memory and back.
@@ -64,6 +65,9 @@ __device__ __forceinline__ float gate_lanes_sum(float v, int log2) {
     if (log2 > 4) v += __shfl_xor(v, 16);
     return v;
 }
+// The gradient of the logit that one of those lanes has; all of them call it together.
+__device__ __forceinline__ float gate_dl(float w, float dw, int log2) { return w * (dw - gate_lanes_sum(w * dw, log2)); }
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 template <int PER>
 struct GateSlots {
     float w[PER], dw[PER];
@@ -87,7 +91,7 @@ struct GateSlots {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int t = (threadIdx.x + i * kGateGradThreads) >> log2;
-            const float dl = w[i] * (dw[i] - gate_lanes_sum(w[i] * dw[i], log2));
+            const float dl = gate_dl(w[i], dw[i], log2);
             if (t >= n || j >= a.k) continue;
             if ((u32)e[i] >= (u32)a.E) report(a.status, MOE_ERR_BAD_ROUTING), e[i] = -1;
             put(i, t, j, e[i], dl);
@@ -192,6 +196,14 @@ __device__ __forceinline__ void cut3_off(float v, u32 *b) {
     b[2] = __float_as_uint(r - __uint_as_float(b[1] << 16)) >> 16;
 }
 
+// What a dWg task meets that is not finite.
+struct GateOdd {
+    int x_first, x_last;    // first and last token whose x has such a number here
+    int sum;                // whether a sum has become a NaN
+    int dl_first, dl_last;  // then: first and last token with such a dl here,
+    u32 again[kGateDwExperts / 32];  // and a bit for each of the experts with an infinite one
+};
+
 // Shape of a dWg task: KT tokens per reduction block; a wavefront has 32 of up to 32 WE experts and all columns, and the 8 / WE
 // wavefronts that have the same multiply a share of the block each.  FEW: at most 8 choices.  (What a step reads from LDS bounds it:
 // three pieces of dl per block of 32 experts, so every wavefront uses them on 64 columns.)
@@ -207,7 +219,7 @@ struct GateDwShape {
     static constexpr int DROW = KT * 2 + 16, XROW = COLS * 2 + 64;
     static constexpr int DPLANE = EPAD * DROW, XPLANE = KT * XROW;
     static constexpr int O_X = 3 * DPLANE, TROW = EPAD + 4, TURN = SHARES * COLS * TROW * 4;
-    static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + 16;
+    static constexpr int O_ODD = O_X + XP * XPLANE > TURN ? O_X + XP * XPLANE : TURN, LDS = O_ODD + (int)sizeof(GateOdd);
     static constexpr int SLOT_LANES = KT * (FEW ? 8 : 32), PER = SLOT_LANES < kGateGradThreads ? 1 : SLOT_LANES / kGateGradThreads;  // passes over a block's slots
     static constexpr int GROUP = FEW ? 2 : 1;          // blocks whose numbers are loaded together
     static constexpr int LANES = COLS / Piece<ET>::N;  // of a row of x, a piece each
@@ -228,7 +240,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     const int t_begin = part * a.dw_tokens, t_end = min(a.T, t_begin + a.dw_tokens);
     const int e_first = group * a.dw_experts, n_e = min(a.E - e_first, a.dw_experts);
     char *xs = smem + C::O_X;
-    int *odd = (int *)(smem + C::O_ODD);  // first and last token whose x has a number here that is not finite
+    GateOdd *odd = (GateOdd *)(smem + C::O_ODD);
     // Loads run a group of blocks ahead, whole groups at a time: a block's tokens are few, and a CU may have one workgroup
     constexpr int GROUP = C::GROUP;
     u32x4_t rows[GROUP][C::NX];
@@ -248,7 +260,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     };
     load_group(t_begin);
     for (int i = tid * 16; i < C::O_X; i += kGateGradThreads * 16) *(u32x4_t *)(smem + i) = u32x4_t{0, 0, 0, 0};
-    if (tid == 0) odd[0] = 0x7fffffff, odd[1] = -1;
+    if (tid == 0) *odd = GateOdd{0x7fffffff, -1, 0, 0x7fffffff, -1, {}};
     const int share = wave / C::WE, e0 = wave % C::WE * 32;
     f32x16_t acc[C::CB];
 #pragma unroll
@@ -290,7 +302,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
         for (int i = 0; i < C::PER; ++i) {
             const int t = (tid + i * kGateGradThreads) >> log2, e = slot.e[i] - e_first;
-            const float dl = slot.w[i] * (slot.dw[i] - gate_lanes_sum(slot.w[i] * slot.dw[i], log2));
+            const float dl = gate_dl(slot.w[i], slot.dw[i], log2);
             const bool there = t < n_tok && j < a.k;
             bad_id |= there && (u32)slot.e[i] >= (u32)a.E;
             old[i] = at[i];
@@ -349,7 +361,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
                     }
                 }
                 const int t = min(t0 + x_tok + m * C::XSTEP, t_end - 1);
-                atomicMin(&odd[0], t), atomicMax(&odd[1], t);
+                atomicMin(&odd->x_first, t), atomicMax(&odd->x_last, t);
             }
             if constexpr (sizeof(ET) == 2)
                 *(u32x4_t *)(to + x_lane * 16) = u32x4_t{piece[m][0].x, piece[m][0].y, piece[m][1].x, piece[m][1].y};
@@ -411,6 +423,7 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
     float *to = out + (size_t)col0 * a.E + e_first;
     int c = tid * step / n_e, e = tid * step - c * n_e;
     const int dc = kGateGradThreads * step / n_e, de = kGateGradThreads * step - dc * n_e;
+    bool odd_sum = false;
     for (int i = tid * step; i < n_out; i += kGateGradThreads * step) {
         const float *from = turn + c * C::TROW + e;
         if (step == 4) {
@@ -418,28 +431,58 @@ __device__ __forceinline__ void gate_dw_task(const GateGradArgs &a, char *smem, 
 #pragma unroll
             for (int h = 1; h < C::SHARES; ++h) sum += *(const f32x4_t *)(from + h * C::COLS * C::TROW);
             *(f32x4_t *)(to + (size_t)c * a.E + e) = sum;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) odd_sum |= sum[q] != sum[q];
         } else {
             float sum = *from;
 #pragma unroll
             for (int h = 1; h < C::SHARES; ++h) sum += from[h * C::COLS * C::TROW];
             to[(size_t)c * a.E + e] = sum;
+            odd_sum |= sum != sum;
         }
         c += dc, e += de;
         if (e >= n_e) e -= n_e, ++c;
     }
+    if (odd_sum) odd->sum = 1;
     sync_stores();
-    if (odd[1] < 0) return;
-    // numbers of x that are not finite: a column's one after the other
-    const int col = col0 + tid;
-    if (tid >= C::COLS || col >= a.d) return;
-    for (int t = odd[0]; t <= odd[1]; ++t) {
+    if (odd->x_last < 0 && !odd->sum) return;
+    if (odd->sum) {  // a NaN among the dl, or an infinite one?
+        const int pass = kGateGradThreads >> log2;
+        int t_first = 0x7fffffff, t_last = -1;
+        for (int t0 = t_begin; t0 < t_end; t0 += pass) {
+            GateSlots<1> slot;
+            slot.load(a, log2, t0, min(pass, t_end - t0));
+            const int t = t0 + (tid >> log2), e = slot.e[0] - e_first;
+            const float dl = gate_dl(slot.w[0], slot.dw[0], log2);
+            if (t >= t_end || (tid & ((1 << log2) - 1)) >= a.k || (u32)e >= (u32)n_e || finite(dl)) continue;
+            t_first = min(t_first, t), t_last = t;
+            if (dl == dl) atomicOr(&odd->again[e >> 5], 1u << (e & 31));
+        }
+        if (t_last >= 0) atomicMin(&odd->dl_first, t_first), atomicMax(&odd->dl_last, t_last);
+        __syncthreads();
+    }
+    if (wave > 0) return;
+    // A lane has a column, and a token's slots lie across the lanes as above.  The sums of an expert with an infinite dl have nothing
+    // finite in them: they start over, from the products that are not finite.
+    static_assert(C::COLS == 64 && kGateDwExperts == 128, "a column per lane, four words of experts");
+    const int col = min(col0 + lane, a.d - 1), j = lane & ((1 << log2) - 1);
+    const bool mine = col0 + lane < a.d, any = (odd->again[0] | odd->again[1] | odd->again[2] | odd->again[3]) != 0u;
+    for (int e = 0; any && e < n_e; ++e)
+        if (mine && (odd->again[e >> 5] >> (e & 31) & 1u)) out[(size_t)col * a.E + e_first + e] = 0.f;
+    const int first = any ? min(odd->x_first, odd->dl_first) : odd->x_first, last = any ? max(odd->x_last, odd->dl_last) : odd->x_last;
+    for (int t = first; t <= last; ++t) {
         const float v = Elem<ET>::load((const ET *)a.x, (size_t)t * a.d + col);
-        if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) continue;
-        const size_t s = (size_t)t * a.k;
-        float mean = 0.f;
-        for (int j = 0; j < a.k; ++j) mean += a.w[s + j] * a.dw[s + j];
-        for (int j = 0; j < a.k; ++j)
-            if ((u32)(a.idx[s + j] - e_first) < (u32)n_e) out[(size_t)col * a.E + a.idx[s + j]] += v * (a.w[s + j] * (a.dw[s + j] - mean));
+        if (!any && !__any(!finite(v))) continue;
+        const u32 s = (u32)t * (u32)a.k + min(j, a.k - 1);
+        const float dl = gate_dl(j < a.k ? a.w[s] : 0.f, j < a.k ? a.dw[s] : 0.f, log2);
+        const int e_mine = a.idx[s] - e_first;
+        for (int i = 0; i < a.k; ++i) {
+            const int e = __shfl(e_mine, i);
+            const float dl_e = __shfl(dl, i);
+            if ((u32)e >= (u32)n_e) continue;
+            const bool again = odd->again[e >> 5] >> (e & 31) & 1u;
+            if (mine && (!finite(v) || (again && !finite(dl_e)))) out[(size_t)col * a.E + e_first + e] += v * dl_e;
+        }
     }
 }
 
