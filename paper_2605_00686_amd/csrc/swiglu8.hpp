@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void k_swiglu_backward(SwigluArgs a) {
             const float s = sigmoid<ET>(g[i]), silu = g[i] * s;
             h[i] = silu * v[i];
             du[i] = dh[i] * silu;
-            dg[i] = dh[i] * v[i] * s * (1.f + g[i] * (1.f - s));
+            dg[i] = dh[i] * (v[i] * (s * (1.f + g[i] * (1.f - s))));  // (dh u may be past the range where a closed gate's gradient is not)
         }
         const size_t row = at.row[u];
         store_piece<ET>(a.dg, row * a.ld + at.c[u], dg);
