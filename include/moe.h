@@ -302,7 +302,7 @@ int moe_unsort_backward(const moe_problem_t *p, const void *dout, const void *ro
                         const float *topk_w, const int32_t *counts, void *drows, float *dtopk_w,
                         int32_t *status_dev, void *stream);
 
-/* Host, pure: bytes of workspace moe_route_backward needs (any content); 0 if the problem is invalid. */
+/* Host, pure: bytes of workspace moe_route_backward needs (any content), 256 where it has nothing to keep there; 0 if the problem is invalid. */
 size_t moe_backward_workspace_bytes(const moe_problem_t *p);
 
 /*

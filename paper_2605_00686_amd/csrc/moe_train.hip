@@ -202,7 +202,7 @@ size_t moe_backward_workspace_bytes(const moe_problem_t *p) {
     if (check_problem(p) != MOE_OK) return 0;
     GateGradArgs a;
     gate_grad_plan(p, &a);
-    return a.dw_parts * a.part_stride * 4;
+    return a.dw_parts > 1 ? a.dw_parts * a.part_stride * 4 : 256;  // (one part's sums go straight to dWg and dgate_bias)
 }
 
 int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx, const float *topk_w,
