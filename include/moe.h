@@ -275,12 +275,14 @@ int moe_combine(const moe_problem_t *p, const void *staging, const uint32_t *fla
  *
  * In these five calls a row is a row of the sorted order that moe_dispatch makes: N rows (p->capacity = 0), or
  * E * capacity rows of which expert e uses the first counts[e] of its own (at most capacity).  inv_perm[s] is the
- * row of slot s; -1 says that the slot has none (a program that drops what an expert has no room for): it adds
- * nothing, and nothing of it is read.  Any other number outside the rows does the same and is reported as
- * MOE_ERR_BAD_ROUTING in status_dev (int32 on the device, may be NULL, written only on failure).  No two slots may
- * have the same row.  `counts` is needed where rows are padded and may be NULL where they are not; unused rows are
- * never read, and come out as zeros.  Sums are fp32; tensors of `dtype`, codes and dWg start on 16
- * bytes (else MOE_ERR_INVALID_ARG).  Outputs may not overlap inputs except where it says so.  The calls keep nothing
+ * row of slot s; -1 says that the slot has none (a program that drops what an expert has no room for, with a dispatch
+ * of its own: moe_dispatch drops nothing): it adds nothing, and neither its weight nor any row counts for it.  Any
+ * other number outside the rows does the same and is reported as MOE_ERR_BAD_ROUTING in status_dev (int32 on the
+ * device, may be NULL, written only on failure).  No two slots may have the same row.  `counts` is needed where rows
+ * are padded and may be NULL where they are not.  What unused rows hold counts for nothing, and they come out as zeros.
+ * (Where there is no row to read, the first one is loaded, used or not, and dropped.)  Sums are fp32; tensors of
+ * `dtype`, codes and dWg start on 16 bytes (else MOE_ERR_INVALID_ARG).  Outputs may not overlap inputs except where it
+ * says so.  The calls keep nothing
  * and clear nothing: the same inputs give the same bits.
  */
 
@@ -335,6 +337,7 @@ int moe_swiglu(const moe_problem_t *p, const void *g, const void *u, int64_t ld,
 /*
  * The gradient of moe_swiglu from what it kept: with g and u as decoded and s = 1 / (1 + exp(-g)),
  * dg = dh u s (1 + g (1 - s)), du = dh g s, and h = g s u once more (for dW2 = h^T dy).
+ * (In fp32: 256 * 2^120, which numbers from 1.9375 * 2^127 on are kept as, is 2^128 and counts as infinite.)
  *   dh [rows, f] dtype in; dg, du [rows, f] dtype out with `ld` elements from one row to the next, as above; h
  *   [rows, f] dtype out, may be NULL.
  */
