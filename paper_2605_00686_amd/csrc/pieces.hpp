@@ -54,11 +54,4 @@ __device__ __forceinline__ void report(int32_t *status, int code) {
     if (status) *status = code;  // (whoever writes, writes the same)
 }
 
-// The row of a slot, or -1: none, or none that exists, which is reported.
-__device__ __forceinline__ int row_of_slot(int row, int rows, int32_t *status) {
-    if ((u32)row < (u32)rows) return row;
-    if (row != -1) report(status, MOE_ERR_BAD_ROUTING);
-    return -1;
-}
-
 }  // namespace moe
