@@ -304,7 +304,8 @@ int moe_unsort_backward(const moe_problem_t *p, const void *dout, const void *ro
                         const float *topk_w, const int32_t *counts, void *drows, float *dtopk_w,
                         int32_t *status_dev, void *stream);
 
-/* Host, pure: bytes of workspace moe_route_backward needs (any content), 256 where it has nothing to keep there; 0 if the problem is invalid. */
+/* Host, pure: bytes of workspace moe_route_backward needs (any content), 256 where it has nothing to keep there; 0 if
+ * the problem is invalid. */
 size_t moe_backward_workspace_bytes(const moe_problem_t *p);
 
 /*
@@ -312,8 +313,10 @@ size_t moe_backward_workspace_bytes(const moe_problem_t *p);
  * (dtopk_w[t,j] - sum_i topk_w[t,i] dtopk_w[t,i]): dx[t] = sum_j dl[t,j] Wg[:,topk_idx[t,j]], one rounding;
  * dWg[:,e] and dgate_bias[e] = the sums of dl x[t] and of dl over the slots that chose e.
  *   dx [T,d] dtype, dWg [d,E] fp32, dgate_bias [E] fp32 out; each may be NULL.  Wg is needed for dx, x for dWg.
- *   The k ids of a token are distinct.  An id outside [0,E) is MOE_ERR_BAD_ROUTING in status_dev; its slot has no gradient (its share of the sum over i
- *   counts).  workspace: moe_backward_workspace_bytes() bytes, 256-byte aligned; needed for dWg and dgate_bias.
+ *   Of dl, and of x in fp32, dWg sees the bits from 2^-133 on (all there are in a number from 2^-110 on).
+ *   The k ids of a token are distinct.  An id outside [0,E) is MOE_ERR_BAD_ROUTING in status_dev; its slot has no
+ *   gradient (its share of the sum over i counts).  workspace: moe_backward_workspace_bytes() bytes, 256-byte aligned;
+ *   needed for dWg and dgate_bias.
  */
 int moe_route_backward(const moe_problem_t *p, const void *x, const void *Wg, const int32_t *topk_idx,
                        const float *topk_w, const float *dtopk_w, void *dx, float *dWg, float *dgate_bias,

@@ -177,7 +177,8 @@ __device__ __forceinline__ void gate_dx_task(const GateGradArgs &a, char *smem, 
 // not finite one is a NaN at least).  Each is the bf16 number nearest to what those before it leave: with 2^e <= |v| < 2^(e+1) the second is
 // 2^(e-8) at most and the third, of the 7 bits that are left, 2^(e-17), so the two products of order 3 come to 2^-24 of the whole at
 // most, of either sign.  (Cut off instead of rounded they came to 2^-21, always towards zero: 0.7 * 2^-24 of a sum on average, however
-// many terms it has.)  Only the first may be rounded past bf16's largest: it stops there.
+// many terms it has.)  Only the first may be rounded past bf16's largest: it stops there.  Bits below 2^-133, bf16's smallest number, are
+// lost: a number from 2^-110 on has all of its own.
 __device__ __forceinline__ void cut3(float lo, float hi, u32 *b) {
     constexpr float kLargest = 0x1.fep127f;
     b[0] = pack_bf16x2(__builtin_amdgcn_fmed3f(lo, -kLargest, kLargest), __builtin_amdgcn_fmed3f(hi, -kLargest, kLargest));
