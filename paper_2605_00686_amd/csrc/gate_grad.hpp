@@ -15,8 +15,9 @@
 // What bounds it: a task's chain per 64 tokens of LDS writes, three barriers and 12 matrix instructions per wavefront, 0.8 us of
 // which the matrix cores are busy 0.3, with one task per CU because every part of the tokens costs its sums (d E fp32) a trip to
 // memory and back.
-// Measured, MI355X, all three gradients: 4096 x 8 of 128 of 2048 21 us, 2048 x 8 of 256 of 7168 35 to 39 us, fp32 256 x 2 of 8 of 512 7.3 us,
-// one token of the first 4.8 us.
+// Measured, MI355X, all three gradients, calls in a row (a call by itself, or traced, takes longer): 4096 x 8 of 128 of 2048 20 us,
+// 2048 x 8 of 256 of 7168 34 us, 16384 x 2 of 8 of 4096 73 us, fp32 256 x 2 of 8 of 512 7.1 us, 9683 x 3 of 3 of 720 19.8 us, 2048 x 8 of 128
+// of 2048 22.5 us; one token's kernel 5.5 us.  More than 128 experts: x is read by each of two groups of them, 65 MB where 33 must be.
 #pragma once
 #include <type_traits>
 

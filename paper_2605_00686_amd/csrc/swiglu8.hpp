@@ -8,7 +8,7 @@
 // Bound by memory: 2 f elements read, f written and 2 f (1 + 1/32) bytes kept per row; backward f elements and the kept bytes read, 3 f
 // elements written.  A lane holds 16 bytes of an input (wider pieces leave half lines per store: fp32 4096 x 1040, gradient, 16.4 us
 // with 8 values per lane, 13.2 with 4), two pieces per thread.  Measured, MI355X, bf16, inputs that change from call to call (the
-// runtime's copy moves 4.7 TB/s there): 32768 rows of 768 36.4 us = 5.6 TB/s, 8192 of 2048 22.3 us, gradient 25.9; 32768 of 14336 635 us = 6.0
+// runtime's copy moves 4.7 TB/s there): 32768 rows of 768 36.2 us = 5.6 TB/s, 8192 of 2048 21.5 us, gradient 25.5; 32768 of 14336 627 us = 6.0
 // TB/s, gradient 808 us = 5.9.
 #pragma once
 #include "pieces.hpp"

@@ -3,8 +3,8 @@
 // token's row, with all its k rows (up to 8) in flight at once, and lives for one trip to memory: many short wavefronts keep more
 // loads in flight than one per token, which also waits for its stores between pieces (4096 x 8 rows of 2048: 46 us, gradient 71).
 // Measured, MI355X, bf16, inputs that change from call to call (where the runtime's copy moves 4.7 TB/s): 4096 x 8 rows of 2048 27.1 us =
-// 5.6 TB/s, their gradient 54.7 us = 5.2; 16384 x 2 of 4096 with an addend 88.5 us = 6.1; fp32 1001 x 6 of 1040 padded to 256 per expert,
-// gradient 16.0 us = 5.0; 16384 x 8 of 64 6.1 us and 7.8; one token's 8 rows of 2048 2.8 us, three trips to memory one behind the other.
+// 5.6 TB/s, their gradient 55.5 us = 5.2; 16384 x 2 of 4096 with an addend 88.2 us = 6.1; fp32 1001 x 6 of 1040 padded to 256 per expert,
+// gradient 16.0 us = 5.0; 16384 x 8 of 64 6.1 us and 7.8; one token's 8 rows of 2048 2.9 us, three trips to memory one behind the other.
 #pragma once
 #include "pieces.hpp"
 
