@@ -348,6 +348,81 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
                         const int32_t *counts, void *dg, void *du, int64_t ld, void *h, void *stream);
 
 /*
+ * The experts' products, for a program that leaves them to the library: with moe_dispatch before and moe_unsort behind, moe_ffn_up and
+ * moe_ffn_down are the layer's forward pass, and moe_ffn_down_backward and moe_ffn_up_backward, between moe_unsort_backward and moe_unsort
+ * without weights, the way back.  (With g and u kept in 8 bits instead: moe_ffn_down_backward to dh, moe_swiglu_backward,
+ * moe_ffn_up_backward.)
+ *
+ * Rows are the sorted order's, as in the five calls above, and counts [E] is needed in both layouts.  Ragged: expert e's rows lie behind those of
+ * the experts before it (offsets = sums of counts); rows behind the last expert's, where the counts do not come to N, are unused.  A count below
+ * zero is zero, one past `capacity` or past N is cut there.  What unused rows hold counts for nothing, and they come out as zeros.  An
+ * expert without rows has gradients of zero.
+ *   x_perm, dx, y, dy [rows, d], h, dh [rows, f] dtype; g, u, dg, du [rows, f] dtype with `ld` elements from one row to the next in all of
+ *   a call, W1, W3 and their gradients [E, d, f] with `ldw` elements from one row to the next and d * ldw from one expert to the next (f, or
+ *   2f where the two are the halves of one [E, d, 2f]); W2, dW2 [E, f, d].  ld, ldw: >= f, whole multiples of 16 bytes; tensors start on 16 bytes.
+ *   Sums are fp32, and what is made of them before an output's one rounding is too.  Outputs may not overlap inputs except where it says so.
+ *   workspace: moe_ffn_workspace_bytes() bytes, 256-byte aligned, any content; calls that may run at the same time have one each.
+ *   The calls keep nothing: the same inputs give the same bits.  A launch of 2^32 threads or more is MOE_ERR_UNSUPPORTED.
+ */
+
+/* Host, pure: bytes of workspace that the four calls need, 0 if the problem is invalid. */
+size_t moe_ffn_workspace_bytes(const moe_problem_t *p);
+
+/* g = x_perm W1[e], u = x_perm W3[e], h = silu(g) u (of the sums, before g and u are rounded).  g and u: both or none may be NULL; h may be
+ * NULL where they are not. */
+int moe_ffn_up(const moe_problem_t *p, const void *x_perm, const void *W1, const void *W3, int64_t ldw, const int32_t *counts,
+               void *g, void *u, int64_t ld, void *h, void *workspace, void *stream);
+
+/* y = h W2[e]. */
+int moe_ffn_down(const moe_problem_t *p, const void *h, const void *W2, const int32_t *counts, void *y, void *workspace,
+                 void *stream);
+
+/*
+ * The gradient of moe_ffn_down, taken on through the activation: dh = dy W2[e]^T; dg = dh u s (1 + g (1 - s)) and du = dh g s with
+ * s = 1 / (1 + exp(-g)), of dh before it is rounded; dW2[e] = h^T dy over the expert's rows.
+ *   dh, dW2: either may be NULL; dg and du: both or none (g and u, which they need, may be NULL then); dg may be g and du may be u.
+ *   W2 is needed for dh, dg and du, h for dW2.
+ */
+int moe_ffn_down_backward(const moe_problem_t *p, const void *dy, const void *W2, const void *h, const void *g, const void *u,
+                          const int32_t *counts, void *dh, void *dg, void *du, int64_t ld, void *dW2, void *workspace,
+                          void *stream);
+
+/*
+ * The gradient of moe_ffn_up's g and u: dx = dg W1[e]^T + du W3[e]^T, dW1[e] = x_perm^T dg and dW3[e] = x_perm^T du over the expert's rows.
+ *   Each output may be NULL; W1, W3 are needed for dx, x_perm for dW1 and dW3, dg for dx and dW1, du for dx and dW3.
+ */
+int moe_ffn_up_backward(const moe_problem_t *p, const void *x_perm, const void *W1, const void *W3, int64_t ldw, const void *dg,
+                        const void *du, int64_t ld, const int32_t *counts, void *dx, void *dW1, void *dW3, void *workspace,
+                        void *stream);
+
+/* One of many tensors: `count` numbers at `in`, in `dtype` (moe_dtype_t), anywhere their type may lie; what is made of them goes to `out`, which
+ * may be `in`.  The list itself is the host's, and read during the call. */
+typedef struct {
+    const void *in;
+    void *out;
+    int64_t count;
+    int32_t dtype, unused;
+} moe_tensor_t;
+
+/* Host, pure: bytes of workspace that moe_grad_norm needs for these tensors, 0 if they are invalid. */
+size_t moe_grad_workspace_bytes(const moe_tensor_t *tensors, int32_t n);
+
+/*
+ * The norm of n tensors together (`out` is not looked at): *sum_squares = the sum of all squares, in 64 bits, *norm = its root (may be NULL).  A
+ * program whose gradients lie on several GPUs adds up the sums of squares before it goes on.
+ *   n may be 0, a tensor may be empty (and NULL then).  sum_squares, norm: on the device.  workspace: moe_grad_workspace_bytes() bytes, 256-byte
+ *   aligned, any content.  The same list of sizes gives the same order of sums.
+ */
+int moe_grad_norm(const moe_tensor_t *tensors, int32_t n, double *sum_squares, float *norm, void *workspace, void *stream);
+
+/*
+ * out = min(1, max_norm / sqrt(*sum_squares)) in, one rounding, for each of n tensors; a norm that is infinite or not a number scales nothing.
+ *   sum_squares: on the device, as moe_grad_norm leaves it.  max_norm: >= 0.  Where the factor is one, a tensor whose `out` is its `in` is not
+ *   touched.  Tensors may not overlap each other.
+ */
+int moe_grad_clip(const moe_tensor_t *tensors, int32_t n, const double *sum_squares, float max_norm, void *stream);
+
+/*
  * Measurement aid, no part of the layer: the rate at which this GPU's matrix cores retire bf16 work when nothing
  * else happens (what the grouped GEMM's "fraction of the MFMA peak" can be held against on a given box; the clock
  * a chip holds under matrix-core load depends on its power limit and on the operand bits).  `workgroups` workgroups

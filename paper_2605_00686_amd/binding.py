@@ -24,7 +24,8 @@ MOE_NUM_STATS = 20
 EXPORTS = ("moe_workspace_bytes", "moe_num_flags", "moe_status_string", "moe_workspace_init", "moe_route",
            "moe_dispatch", "moe_dispatch_noalloc", "moe_megakernel_forward", "moe_combine", "moe_probe_mfma",
            "moe_probe_stream", "moe_unsort", "moe_unsort_backward", "moe_backward_workspace_bytes", "moe_route_backward",
-           "moe_swiglu", "moe_swiglu_backward")
+           "moe_swiglu", "moe_swiglu_backward", "moe_ffn_workspace_bytes", "moe_ffn_up", "moe_ffn_down", "moe_ffn_down_backward",
+           "moe_ffn_up_backward", "moe_grad_workspace_bytes", "moe_grad_norm", "moe_grad_clip")
 
 
 class MoeProblem(ctypes.Structure):
@@ -35,6 +36,11 @@ class MoeProblem(ctypes.Structure):
                                                                                  ("capacity", ctypes.c_int32),
                                                                                  ("wait_ticks", ctypes.c_uint32),
                                                                                  ("fuse_ffn", ctypes.c_int32)]
+
+
+class MoeTensor(ctypes.Structure):
+    _fields_ = [("inp", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("unused", ctypes.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -69,9 +75,21 @@ _lib.moe_backward_workspace_bytes.argtypes = [_pp]
 _lib.moe_route_backward.argtypes = [_pp] + [_vp] * 11
 _lib.moe_swiglu.argtypes = [_pp, _vp, _vp, ctypes.c_int64] + [_vp] * 5
 _lib.moe_swiglu_backward.argtypes = [_pp] + [_vp] * 6 + [ctypes.c_int64, _vp, _vp]
+_lib.moe_ffn_workspace_bytes.restype = ctypes.c_size_t
+_lib.moe_ffn_workspace_bytes.argtypes = [_pp]
+_lib.moe_ffn_up.argtypes = [_pp, _vp, _vp, _vp, ctypes.c_int64, _vp, _vp, _vp, ctypes.c_int64, _vp, _vp, _vp]
+_lib.moe_ffn_down.argtypes = [_pp] + [_vp] * 6
+_lib.moe_ffn_down_backward.argtypes = [_pp] + [_vp] * 9 + [ctypes.c_int64] + [_vp] * 3
+_lib.moe_ffn_up_backward.argtypes = [_pp, _vp, _vp, _vp, ctypes.c_int64, _vp, _vp, ctypes.c_int64] + [_vp] * 6
+_tp = ctypes.POINTER(MoeTensor)
+_lib.moe_grad_workspace_bytes.restype = ctypes.c_size_t
+_lib.moe_grad_workspace_bytes.argtypes = [_tp, ctypes.c_int32]
+_lib.moe_grad_norm.argtypes = [_tp, ctypes.c_int32] + [_vp] * 4
+_lib.moe_grad_clip.argtypes = [_tp, ctypes.c_int32, _vp, ctypes.c_float, _vp]
 for _n in ("moe_workspace_init", "moe_route", "moe_dispatch", "moe_dispatch_noalloc", "moe_megakernel_forward",
            "moe_combine", "moe_probe_mfma", "moe_probe_stream", "moe_unsort", "moe_unsort_backward", "moe_route_backward",
-           "moe_swiglu", "moe_swiglu_backward"):
+           "moe_swiglu", "moe_swiglu_backward", "moe_ffn_up", "moe_ffn_down", "moe_ffn_down_backward", "moe_ffn_up_backward",
+           "moe_grad_norm", "moe_grad_clip"):
     getattr(_lib, _n).restype = ctypes.c_int
 
 
@@ -190,6 +208,86 @@ def moe_swiglu_backward(p, dh, codes, scales, counts, dg, du, h, stream=None):
     gp, up, ld = _row_ptrs(dg, du)
     _check(_lib.moe_swiglu_backward(ctypes.byref(p), _ptr(dh), _ptr(codes), _ptr(scales), _ptr(counts), gp, up, ld, _ptr(h),
                                     _stream(stream)), "moe_swiglu_backward")
+
+
+def moe_ffn_workspace_bytes(p: MoeProblem) -> int:
+    return int(_lib.moe_ffn_workspace_bytes(ctypes.byref(p)))
+
+
+def _like_rows(*tensors):
+    """[rows, f] tensors or views (or None) whose rows are the same number of elements apart: that number, and their addresses."""
+    given = [t for t in tensors if t is not None]
+    if not given:
+        return (0,) + (None,) * len(tensors)
+    (rows, f), ld = given[0].shape, given[0].stride(0)
+    for t in given:
+        assert t.is_cuda and t.shape == given[0].shape and (f == 1 or t.stride(1) == 1), "device tensors, rows of one piece"
+        assert rows == 1 or t.stride(0) == ld, "rows the same number of elements apart"
+    return (ld if rows > 1 else f,) + tuple(None if t is None else t.data_ptr() for t in tensors)
+
+
+def _like_matrices(*tensors):
+    """[E, d, f] tensors or views (or None), matrix behind matrix, whose rows are the same number of elements apart: as _like_rows."""
+    for t in tensors:
+        if t is not None:
+            assert t.dim() == 3 and (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1)), "matrix behind matrix"
+    return _like_rows(*(None if t is None else t.flatten(0, 1) for t in tensors))
+
+
+def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
+    ldw, w1, w3 = _like_matrices(W1, W3)
+    ld, gp, up = _like_rows(g, u)
+    _check(_lib.moe_ffn_up(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, _ptr(counts), gp, up, ld, _ptr(h), _ptr(workspace),
+                           _stream(stream)), "moe_ffn_up")
+
+
+def moe_ffn_down(p, h, W2, counts, y, workspace, stream=None):
+    _check(_lib.moe_ffn_down(ctypes.byref(p), _ptr(h), _ptr(W2), _ptr(counts), _ptr(y), _ptr(workspace), _stream(stream)),
+           "moe_ffn_down")
+
+
+def moe_ffn_down_backward(p, dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace, stream=None):
+    ld, gp, up, dgp, dup = _like_rows(g, u, dg, du)
+    _check(_lib.moe_ffn_down_backward(ctypes.byref(p), _ptr(dy), _ptr(W2), _ptr(h), gp, up, _ptr(counts), _ptr(dh), dgp, dup, ld,
+                                      _ptr(dW2), _ptr(workspace), _stream(stream)), "moe_ffn_down_backward")
+
+
+def moe_ffn_up_backward(p, x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace, stream=None):
+    ldw, w1, w3, dw1, dw3 = _like_matrices(W1, W3, dW1, dW3)
+    ld, dgp, dup = _like_rows(dg, du)
+    _check(_lib.moe_ffn_up_backward(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, dgp, dup, ld, _ptr(counts), _ptr(dx), dw1, dw3,
+                                    _ptr(workspace), _stream(stream)), "moe_ffn_up_backward")
+
+
+class TensorList:
+    """Gradients, and where they go, as moe_grad_norm and moe_grad_clip take them; holds the tensors."""
+
+    def __init__(self, ins, outs):
+        assert len(ins) == len(outs), "an output for every input"
+        for i, o in zip(ins, outs):
+            assert i.is_cuda and i.is_contiguous() and o.is_contiguous() and o.device == i.device, "device tensors, contiguous"
+            assert i.dtype == o.dtype and i.numel() == o.numel() and i.dtype in (torch.float32, torch.bfloat16), "fp32 or bf16, both the same"
+        self.tensors = list(ins), list(outs)
+        self.n = len(self.tensors[0])
+        self.array = (MoeTensor * max(1, self.n))(*(MoeTensor(i.data_ptr(), o.data_ptr(), i.numel(), MOE_DT_F32 if i.dtype == torch.float32 else MOE_DT_BF16, 0)
+                                                    for i, o in zip(*self.tensors)))
+
+
+def tensor_list(ins, outs=None) -> TensorList:
+    """What moe_grad_norm and moe_grad_clip work on; without `outs` the tensors themselves are scaled."""
+    return TensorList(ins, ins if outs is None else outs)
+
+
+def moe_grad_workspace_bytes(tensors: TensorList) -> int:
+    return int(_lib.moe_grad_workspace_bytes(tensors.array, tensors.n))
+
+
+def moe_grad_norm(tensors, sum_squares, norm, workspace, stream=None):
+    _check(_lib.moe_grad_norm(tensors.array, tensors.n, _ptr(sum_squares), _ptr(norm), _ptr(workspace), _stream(stream)), "moe_grad_norm")
+
+
+def moe_grad_clip(tensors, sum_squares, max_norm, stream=None):
+    _check(_lib.moe_grad_clip(tensors.array, tensors.n, _ptr(sum_squares), float(max_norm), _stream(stream)), "moe_grad_clip")
 
 
 def moe_probe_mfma(frag, iters, workgroups, sink, stream=None):

@@ -1,0 +1,157 @@
+// C ABI of the experts' products as calls of their own: argument checks and launches.  Declarations and contracts live in include/moe.h.
+#include <hip/hip_runtime.h>
+
+#include "ffn.hpp"
+#include "problem.hpp"
+
+using namespace moe;
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+static int rows_of(const moe_problem_t *p) { return p->capacity > 0 ? p->E * p->capacity : p->T * p->k; }
+static int elem_bytes(const moe_problem_t *p) { return p->dtype == MOE_DT_F32 ? 4 : 2; }
+static bool bad_stride(const moe_problem_t *p, int64_t ld, int cols) { return ld < cols || ld * elem_bytes(p) % 16 != 0; }
+
+template <class T, FfnOp OP>
+static int launch(FfnArgs a, hipStream_t st) {
+    constexpr int COLS = OP == kFfnUp ? T::BN / 2 : T::BN;
+    a.nt = (a.N + COLS - 1) / COLS * (OP == kFfnDw && a.o1 ? 2 : 1);
+    a.mt = (a.M + T::BM - 1) / T::BM;
+    // as many workgroups as there can be tiles, whatever the counts are: a row block per BM rows and one more per expert (ragged: and for
+    // the rows behind the last one)
+    size_t blocks;
+    if (OP == kFfnDw)
+        blocks = (size_t)a.E * a.mt;
+    else if (a.capacity)
+        blocks = (size_t)a.E * ((a.capacity + T::BM - 1) / T::BM);
+    else
+        blocks = (size_t)a.rows / T::BM + (size_t)(a.E < a.rows ? a.E : a.rows) + 1;
+    const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues;
+    if (tiles * T::THREADS >= (size_t)1 << 32) return MOE_ERR_UNSUPPORTED;
+    if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
+    hipLaunchKernelGGL((k_ffn<T, OP>), dim3((unsigned)tiles), dim3(T::THREADS), T::SMEM, st, a);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+template <typename ET, FfnOp OP>
+static int pick(const FfnArgs &a, int slots, hipStream_t st) {
+    if constexpr (sizeof(ET) == 4) {
+        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 2, 2, 2, 4>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 4>, OP>(a, st);
+    } else {
+        if (slots / a.E > 160) return launch<FfnTile<ET, 2, 4, 4, 2, 4>, OP>(a, st);
+        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 4, 2, 2, 3>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 4>, OP>(a, st);
+    }
+}
+template <typename ET>
+static int pick_dw(const FfnArgs &a, hipStream_t st) {
+    if constexpr (sizeof(ET) == 4)
+        return launch<FfnTile<ET, 2, 2, 2, 2, 4>, kFfnDw>(a, st);
+    else
+        return launch<FfnTile<ET, 2, 4, 4, 2, 4>, kFfnDw>(a, st);
+}
+template <FfnOp OP>
+static int pick(const moe_problem_t *p, const FfnArgs &a, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if constexpr (OP == kFfnDw)
+        return p->dtype == MOE_DT_F32 ? pick_dw<float>(a, st) : pick_dw<bf16_t>(a, st);
+    else
+        return p->dtype == MOE_DT_F32 ? pick<float, OP>(a, p->T * p->k, st) : pick<bf16_t, OP>(a, p->T * p->k, st);
+}
+static FfnArgs args_of(const moe_problem_t *p, const int32_t *counts) {
+    FfnArgs a = {};
+    a.E = p->E; a.rows = rows_of(p); a.capacity = p->capacity; a.counts = counts;
+    return a;
+}
+
+extern "C" {
+
+size_t moe_ffn_workspace_bytes(const moe_problem_t *p) { return check_problem(p) == MOE_OK ? 256 : 0; }
+
+static int check_workspace(const void *ws) { return !ws || ((uintptr_t)ws & 255) != 0 ? MOE_ERR_WORKSPACE : MOE_OK; }
+
+int moe_ffn_up(const moe_problem_t *p, const void *x_perm, const void *W1, const void *W3, int64_t ldw, const int32_t *counts, void *g, void *u,
+               int64_t ld, void *h, void *workspace, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!x_perm || !W1 || !W3 || !counts || !g != !u || (!g && !h)) return MOE_ERR_INVALID_ARG;
+    if (bad_stride(p, ldw, p->f) || (g && bad_stride(p, ld, p->f))) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(x_perm) || !aligned16(W1) || !aligned16(W3) || !aligned16(g) || !aligned16(u) || !aligned16(h)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace))) return rc;
+    FfnArgs a = args_of(p, counts);
+    a.N = p->f; a.K = p->d;
+    a.A0 = x_perm; a.lda = p->d;
+    a.B0 = W1; a.B1 = W3; a.ldb = ldw; a.eb = (long long)p->d * ldw;
+    a.o0 = g; a.o1 = u; a.ldo = ld; a.o2 = h;
+    return pick<kFfnUp>(p, a, stream);
+}
+
+int moe_ffn_down(const moe_problem_t *p, const void *h, const void *W2, const int32_t *counts, void *y, void *workspace, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!h || !W2 || !counts || !y) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(h) || !aligned16(W2) || !aligned16(y)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace))) return rc;
+    FfnArgs a = args_of(p, counts);
+    a.N = p->d; a.K = p->f;
+    a.A0 = h; a.lda = p->f;
+    a.B0 = W2; a.ldb = p->d; a.eb = (long long)p->f * p->d;
+    a.o0 = y;
+    return pick<kFfnDown>(p, a, stream);
+}
+
+int moe_ffn_down_backward(const moe_problem_t *p, const void *dy, const void *W2, const void *h, const void *g, const void *u, const int32_t *counts,
+                          void *dh, void *dg, void *du, int64_t ld, void *dW2, void *workspace, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!dy || !counts || !dg != !du || (!dh && !dg && !dW2)) return MOE_ERR_INVALID_ARG;
+    if (((dh || dg) && !W2) || (dg && (!g || !u)) || (dW2 && !h)) return MOE_ERR_INVALID_ARG;
+    if (dg && bad_stride(p, ld, p->f)) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(dy) || !aligned16(W2) || !aligned16(h) || !aligned16(g) || !aligned16(u) || !aligned16(dh) || !aligned16(dg) || !aligned16(du) ||
+        !aligned16(dW2))
+        return MOE_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace))) return rc;
+    if (dh || dg) {
+        FfnArgs a = args_of(p, counts);
+        a.N = p->f; a.K = p->d;
+        a.A0 = dy; a.lda = p->d;
+        a.B0 = W2; a.ldb = p->d; a.eb = (long long)p->f * p->d;
+        a.g = g; a.u = u; a.ldg = ld;
+        a.o0 = dg; a.o1 = du; a.ldo = ld; a.o2 = dh;
+        if ((rc = pick<kFfnDh>(p, a, stream))) return rc;
+    }
+    if (!dW2) return MOE_OK;
+    FfnArgs a = args_of(p, counts);
+    a.M = p->f; a.N = p->d;
+    a.A0 = h; a.lda = p->f;
+    a.B0 = dy; a.ldb = p->d;
+    a.o0 = dW2; a.ldo = p->d; a.eo = (long long)p->f * p->d;
+    return pick<kFfnDw>(p, a, stream);
+}
+
+int moe_ffn_up_backward(const moe_problem_t *p, const void *x_perm, const void *W1, const void *W3, int64_t ldw, const void *dg, const void *du,
+                        int64_t ld, const int32_t *counts, void *dx, void *dW1, void *dW3, void *workspace, void *stream) {
+    int rc = check_problem(p);
+    if (rc) return rc;
+    if (!counts || (!dx && !dW1 && !dW3)) return MOE_ERR_INVALID_ARG;
+    if ((dx && (!W1 || !W3)) || ((dx || dW1) && !dg) || ((dx || dW3) && !du) || ((dW1 || dW3) && !x_perm)) return MOE_ERR_INVALID_ARG;
+    if (bad_stride(p, ldw, p->f) || bad_stride(p, ld, p->f)) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(x_perm) || !aligned16(W1) || !aligned16(W3) || !aligned16(dg) || !aligned16(du) || !aligned16(dx) || !aligned16(dW1) || !aligned16(dW3))
+        return MOE_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace))) return rc;
+    if (dx) {
+        FfnArgs a = args_of(p, counts);
+        a.N = p->d; a.K = p->f;
+        a.A0 = dg; a.A1 = du; a.lda = ld;
+        a.B0 = W1; a.B1 = W3; a.ldb = ldw; a.eb = (long long)p->d * ldw;
+        a.o0 = dx;
+        if ((rc = pick<kFfnDx>(p, a, stream))) return rc;
+    }
+    if (!dW1 && !dW3) return MOE_OK;
+    FfnArgs a = args_of(p, counts);
+    a.M = p->d; a.N = p->f;
+    a.A0 = x_perm; a.lda = p->d;
+    a.B0 = dW1 ? dg : du; a.B1 = du; a.ldb = ld;
+    a.o0 = dW1 ? dW1 : dW3; a.o1 = dW1 ? dW3 : nullptr; a.ldo = ldw; a.eo = (long long)p->d * ldw;
+    return pick<kFfnDw>(p, a, stream);
+}
+
+}  // extern "C"
