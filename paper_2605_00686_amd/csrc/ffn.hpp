@@ -10,11 +10,15 @@
 // All are tiles of C[m,n] = sum over k of A(m,k) B(k,n) on the matrix cores; what differs is which of an operand's indices is contiguous
 // in memory, k ("KC" below) or the other one, and what is done with a tile's sums.  Sums are fp32, outputs are rounded once.
 #pragma once
+#include <type_traits>
+
 #include "gemm_bf16.hpp"
 #include "pieces.hpp"
 #include "swiglu8.hpp"
 
 namespace moe {
+
+typedef long long i64;
 
 enum FfnOp { kFfnUp, kFfnDown, kFfnDh, kFfnDx, kFfnDw };
 
@@ -30,20 +34,24 @@ struct FfnArgs {
     void *o0, *o1, *o2;
 };
 
-// One operand's stage: R indices x 64 bytes of the reduction (32 steps of bf16, 16 of fp32), R * 64 bytes of LDS.
-//   KC:     [R][64 bytes]
+constexpr int kDwStart = 96;  // rows of reduction that the start and end of a tile of dw cost as much as
+
+// One operand's stage: R indices x KB bytes of the reduction (64: 32 steps of bf16, 16 of fp32), R * KB bytes of LDS.
+//   KC:     [R][KB bytes]
 //   not KC: [steps][R]
 // A load instruction moves 64 x 16 bytes into consecutive LDS, so a lane's place there says which piece of 16 bytes it fetches: pieces are
 // placed so that the reads below meet no bank twice.
-template <typename ET, int R, bool KC, int WAVES>
+template <typename ET, int R, bool KC_, int KB, int WAVES>
 struct Operand {
-    static constexpr int SZ = sizeof(ET), STEPS = 64 / SZ, BYTES = R * 64;
+    static constexpr bool KC = KC_;
+    static constexpr int SZ = sizeof(ET), STEPS = KB / SZ, BYTES = R * KB;
     static constexpr int INSTR = BYTES / 1024, PER_WAVE = (INSTR + WAVES - 1) / WAVES;
-    static constexpr int ROW = KC ? 64 : R * SZ;  // bytes of a row in LDS
+    static constexpr int ROW = KC ? KB : R * SZ;  // bytes of a row in LDS
     static constexpr int PIECES = ROW / 16, ROWS_PER_INSTR = 64 / PIECES;
+    static constexpr int READS = KC ? 1 : SZ == 2 ? 2 : 4;  // LDS instructions per fragment
     static_assert(KC || SZ * R >= 128, "rows the placement is made for");
     static __device__ __forceinline__ int place(int row, int c) {  // (its own inverse)
-        if (KC) return c ^ ((row >> 2) & 3);
+        if (KC) return c ^ (KB == 64 ? (row >> 2) & 3 : (row >> 1) & 7);
         if (SZ == 4) return c ^ (((row >> 2) & 1) << 3);
         return R >= 128 ? c ^ ((row & 3) << 2) : c ^ (((row >> 1) & 1) << 2);
     }
@@ -58,26 +66,29 @@ __device__ __forceinline__ void load_to_lds(const char *src, u32 lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src) : "m0");
 }
 
-// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts, NS stages.
-template <typename ET_, int MB_, int NB_, int WM_, int WN_, int NS_>
-struct FfnTile {
-    typedef ET_ ET;
-    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, NS = NS_, WAVES = WM * WN, THREADS = 64 * WAVES;
-    static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * 64;
-    // a wavefront's sums on their way out: 32 rows x 64 columns of fp32, two of them (up: g and u)
-    static constexpr int OUT_ROW = 64 * 4 + 16, OUT_HALF = 32 * OUT_ROW, OUT = 2 * OUT_HALF;
-    static constexpr int HEAD = 256;  // bytes in front of the stages: which rows the workgroup has
-    static constexpr int SMEM = HEAD + (NS * STAGE > WAVES * OUT ? NS * STAGE : WAVES * OUT);
-    static_assert(NB == 2 || NB == 4, "columns of a wavefront");
-};
-
-// Rows that a workgroup has: [begin, begin + used) are expert e's, those up to begin + extent belong to nobody.
+// A workgroup's row block, or dw's expert: rows [begin, begin + used) are expert e's, those up to begin + extent nobody's.
 struct Segment {
     int e, begin, used, extent, block;
 };
-struct FfnHead {
+// Where every expert's rows lie, as a workgroup finds out once.
+struct FfnTables {
     u64 sum[16];
-    Segment seg;
+    int begin[kMaxExperts + 1], used[kMaxExperts];  // begin[E]: behind the last one's (ragged)
+    int first[kMaxExperts + 1];  // first row block of an expert, of the rows of nobody behind the last (ragged); dw: rows before, and kDwStart for each expert
+    int n_tiles;
+};
+
+// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts, stages of KB bytes of the reduction, NS of them.
+template <typename ET_, int MB_, int NB_, int WM_, int WN_, int KB_, int NS_>
+struct FfnTile {
+    typedef ET_ ET;
+    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KB = KB_, NS = NS_, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * KB;
+    // a block of a wavefront's sums on its way out, 32 rows x 32 columns of fp32
+    static constexpr int OUT_ROW = 32 * 4 + 16, OUT = 32 * OUT_ROW;
+    static constexpr int AT_OUT = NS * STAGE, AT_TABLES = AT_OUT + WAVES * OUT;
+    static constexpr int SMEM = AT_TABLES + (int)sizeof(FfnTables);
+    static_assert(SMEM <= 160 * 1024, "LDS");
 };
 
 template <int WAVES>
@@ -100,12 +111,35 @@ __device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  //
     return v + before;
 }
 
-// Tile number `id` of the launch -> which one of `n` this workgroup takes: workgroups go round the eight XCDs, and each XCD takes a stretch of
-// the tiles, whose neighbours read the same operands, from its own L2.
-__device__ __forceinline__ int tile_of_xcd(int id, int n) {
-    const int each = (n + kTileQueues - 1) / kTileQueues, t = (id % kTileQueues) * each + id / kTileQueues;
-    return id / kTileQueues < each && t < n ? t : -1;
+// The tables, by all threads.  Ragged: thread i has expert i.
+template <class T, bool DW>
+__device__ __forceinline__ void make_tables(const FfnArgs &a, FfnTables *t) {
+    const int tid = threadIdx.x;
+    const int n = tid < a.E ? max(a.counts[tid], 0) : 0;
+    int begin, used, blocks;
+    if (a.capacity) {
+        begin = tid * a.capacity, used = min(n, a.capacity), blocks = (a.capacity + T::BM - 1) / T::BM;
+    } else {
+        u64 all;
+        const u64 end = scan_workgroup<T::WAVES>((u64)min(n, a.rows), t->sum, &all);
+        begin = (int)min(end - min(n, a.rows), (u64)a.rows), used = (int)min(end, (u64)a.rows) - begin, blocks = (used + T::BM - 1) / T::BM;
+        if (tid == 0) t->begin[a.E] = (int)min(all, (u64)a.rows);
+    }
+    if (DW) blocks = used + kDwStart;
+    if (tid >= a.E) blocks = 0;
+    u64 all;
+    const int to = (int)scan_workgroup<T::WAVES>((u64)blocks, t->sum + 8, &all);
+    if (tid < a.E) t->begin[tid] = begin, t->used[tid] = used, t->first[tid] = to - blocks;
+    if (tid == 0) t->first[a.E] = (int)all;
+    __syncthreads();
 }
+// The last of the E + 1 ascending numbers that is `v` or less (the first one is).
+__device__ __forceinline__ int last_up_to(const int *list, int n, int v) {
+    int found = 0;
+    for (int i = threadIdx.x & 63; i - (int)(threadIdx.x & 63) < n; i += 64) found += __popcll(__ballot(i < n && list[i] <= v));
+    return uniform(found) - 1;
+}
+
 // Tiles in groups of kTileGroup rows of tiles, column by column inside a group.
 constexpr int kTileGroup = 4;
 __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r, int *c) {
@@ -114,60 +148,27 @@ __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r
     *r = first + in % n, *c = in / n;
 }
 
-// The workgroup's row block and column tile; false: none.  Every expert has ceil(rows / BM) row blocks of its own, and the rows of nobody
-// (padded: behind an expert's; ragged: behind the last one's) are in row blocks too, whose results are zeros.
-template <class T>
-__device__ __forceinline__ bool find_rows(const FfnArgs &a, FfnHead *h, Segment *s, int *col) {
-    const int tid = threadIdx.x;
-    int r;
-    if (a.capacity) {
-        const int per = (a.capacity + T::BM - 1) / T::BM, t = tile_of_xcd(blockIdx.x, a.E * per * a.nt);
-        if (t < 0) return false;
-        tile_in_groups(t, a.E * per, a.nt, &r, col);
-        s->e = r / per, s->block = r - s->e * per;
-        s->begin = s->e * a.capacity, s->extent = a.capacity, s->used = min(max(a.counts[s->e], 0), a.capacity);
-        return true;
-    }
-    // ragged: thread i has expert i
-    u64 all, blocks;
-    const u64 n = tid < a.E ? (u64)min(max(a.counts[tid], 0), a.rows) : 0;
-    const u64 end = scan_workgroup<T::WAVES>(n, h->sum, &all);
-    const int last = (int)min(all, (u64)a.rows), begin = (int)min(end - n, (u64)a.rows), used = (int)min(end, (u64)a.rows) - begin;
-    const int mine = (used + T::BM - 1) / T::BM;
-    const int to = (int)scan_workgroup<T::WAVES>((u64)mine, h->sum + 8, &blocks), rest = (a.rows - last + T::BM - 1) / T::BM;
-    const int t = tile_of_xcd(blockIdx.x, ((int)blocks + rest) * a.nt);
-    if (t < 0) return false;
-    tile_in_groups(t, (int)blocks + rest, a.nt, &r, col);
-    if (r >= to - mine && r < to) h->seg = Segment{tid, begin, used, used, r - (to - mine)};
-    if (r >= (int)blocks && tid == 0) h->seg = Segment{0, last, 0, a.rows - last, r - (int)blocks};
-    __syncthreads();
-    *s = h->seg;
-    return true;
-}
-
-// dw: the workgroup's expert and tile.
-template <class T>
-__device__ __forceinline__ bool find_matrix(const FfnArgs &a, FfnHead *h, Segment *s, int *row, int *col) {
-    const int per = a.mt * a.nt, t = tile_of_xcd(blockIdx.x, a.E * per), tid = threadIdx.x;
-    if (t < 0) return false;
-    s->e = t / per, s->block = 0;
-    tile_in_groups(t - s->e * per, a.mt, a.nt, row, col);
-    if (a.capacity) {
-        s->begin = s->e * a.capacity, s->extent = s->used = min(max(a.counts[s->e], 0), a.capacity);
-        return true;
-    }
-    u64 before = 0;
-    for (int i = tid; i < s->e; i += T::THREADS) before += (u64)max(a.counts[i], 0);
+// Workgroups go round the eight XCDs; each XCD takes a stretch of the tiles, whose neighbours read the same operands, from its own L2: tiles
+// [from, to), workgroup number `id` / 8 of the XCD every `step`-th.
+struct TileRange {
+    int next, to, step;
+};
+template <bool DW>
+__device__ __forceinline__ TileRange tiles_of(const FfnArgs &a, const FfnTables *t, int row_blocks) {
+    const int x = blockIdx.x % kTileQueues;
+    int edge[2];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
-    if ((tid & 63) == 0) h->sum[tid >> 6] = before;
-    __syncthreads();
-    before = 0;
-#pragma unroll
-    for (int w = 0; w < T::WAVES; ++w) before += h->sum[w];
-    s->begin = (int)min(before, (u64)a.rows);
-    s->extent = s->used = min(max(a.counts[s->e], 0), a.rows - s->begin);
-    return true;
+    for (int i = 0; i < 2; ++i) {
+        if (DW) {
+            // stretches of about the same work: a tile is worth its expert's rows and kDwStart
+            const u64 at = (u64)(x + i) * (u32)t->first[a.E];
+            const int e = min(last_up_to(t->first, a.E + 1, (int)(at / kTileQueues)), a.E - 1), per = a.mt * a.nt;
+            edge[i] = x + i == kTileQueues ? a.E * per : e * per + (int)((at - (u64)kTileQueues * t->first[e]) * per / (u64)(kTileQueues * (t->used[e] + kDwStart)));
+        } else {
+            edge[i] = (int)((i64)row_blocks * a.nt * (x + i) / kTileQueues);
+        }
+    }
+    return TileRange{edge[0] + (int)(blockIdx.x / kTileQueues), edge[1], (int)(gridDim.x / kTileQueues)};
 }
 
 // The fragments of N blocks of an operand for step `kk` (32 bytes of the reduction) of a stage: lane l has index l & 31 of a block and the
@@ -176,9 +177,9 @@ template <class O, int N>
 __device__ __forceinline__ void read_frags(const char *stage, int kk, const int (&at)[N], int lane, u32x4_t (&f)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if constexpr (O::PIECES == 4) {
+        if constexpr (O::KC) {
             const int r = at[i] + (lane & 31);
-            f[i] = *(const u32x4_t *)(stage + r * 64 + O::place(r, kk * 2 + (lane >> 5)) * 16);
+            f[i] = *(const u32x4_t *)(stage + r * O::ROW + O::place(r, kk * 2 + (lane >> 5)) * 16);
         } else if constexpr (O::SZ == 2) {
             // (each 16 lanes read 4 steps x 16 indices and hand them out transposed)
             const int c = at[i] + 16 * ((lane >> 4) & 1) + 4 * (lane & 3), k = 8 * (lane >> 5) + ((lane & 15) >> 2);
@@ -204,229 +205,371 @@ __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32
     }
 }
 
-template <typename ET>
-__device__ __forceinline__ void store8(void *p, size_t i, const float *v) {
-    typedef Piece<ET> P;
-#pragma unroll
-    for (int j = 0; j < 8; j += P::N) *(u32x4_t *)((ET *)p + i + j) = P::pack(v + j);
-}
-template <typename ET>
-__device__ __forceinline__ void load8(const void *p, size_t i, float *v) {
-    typedef Piece<ET> P;
-#pragma unroll
-    for (int j = 0; j < 8; j += P::N) P::unpack(*(const u32x4_t *)((const ET *)p + i + j), v + j);
-}
-
 template <class T, FfnOp OP>
 __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     typedef typename T::ET ET;
-    constexpr bool AK = OP != kFfnDw, BK = OP == kFfnDh || OP == kFfnDx, GATED = OP == kFfnUp;
-    typedef Operand<ET, T::BM, AK, T::WAVES> OA;
-    typedef Operand<ET, T::BN, BK, T::WAVES> OB;
+    constexpr bool DW = OP == kFfnDw, AK = !DW, BK = OP == kFfnDh || OP == kFfnDx, GATED = OP == kFfnUp;
+    typedef Operand<ET, T::BM, AK, T::KB, T::WAVES> OA;
+    typedef Operand<ET, T::BN, BK, T::KB, T::WAVES> OB;
     constexpr int LPS = OA::PER_WAVE + OB::PER_WAVE, SZ = sizeof(ET), STEPS = OA::STEPS, PIECE = 16 / SZ;
     constexpr int COLS = GATED ? T::BN / 2 : T::BN;  // columns of a matrix per tile
+    static_assert(T::THREADS >= kMaxExperts, "a thread per expert");
+    static_assert(!GATED || T::NB % 2 == 0, "g and u of the same columns");
     extern __shared__ __align__(128) char smem[];
-    FfnHead *head = (FfnHead *)smem;
-    static_assert(sizeof(FfnHead) <= T::HEAD, "head");
-    char *stages = smem + T::HEAD;
-
-    Segment s;
-    int row0, col;
-    if constexpr (OP == kFfnDw) {
-        int row;
-        if (!find_matrix<T>(a, head, &s, &row, &col)) return;
-        row0 = row * T::BM;
-    } else {
-        if (!find_rows<T>(a, head, &s, &col)) return;
-        row0 = s.block * T::BM;
-    }
-    // dw: column tiles of the second matrix behind those of the first
-    const int per_matrix = (a.N + COLS - 1) / COLS;
-    const int matrix = OP == kFfnDw ? col / per_matrix : 0;
-    const int n0 = (col - matrix * per_matrix) * COLS;
+    char *stages = smem;
+    const FfnTables *tables = (const FfnTables *)(smem + T::AT_TABLES);
+    make_tables<T, DW>(a, (FfnTables *)tables);
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
-
-    f32x16_t acc[T::MB][T::NB];
-#pragma unroll
-    for (int mb = 0; mb < T::MB; ++mb)
-#pragma unroll
-        for (int nb = 0; nb < T::NB; ++nb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[mb][nb][v] = 0.f;
+    const int used_blocks = tables->first[a.E];
+    const int row_blocks = uniform(DW || a.capacity ? used_blocks : used_blocks + (a.rows - tables->begin[a.E] + T::BM - 1) / T::BM);
+    TileRange range = tiles_of<DW>(a, tables, row_blocks);
+    if (range.next >= range.to) return;
 
     const int half = a.K / STEPS;  // stages of a pair of operands
-    const int nk = OP == kFfnDw ? (s.used + STEPS - 1) / STEPS : row0 >= s.used ? 0 : OP == kFfnDx ? 2 * half : half;
-    if (nk) {
-        const char *ap[OA::PER_WAVE], *bp[OB::PER_WAVE];
-        const size_t lda = (size_t)a.lda * SZ, ldb = (size_t)a.ldb * SZ;
-        const char *A = (const char *)a.A0, *B = (const char *)(OP == kFfnDw && matrix ? a.B1 : a.B0);
+    const int per_matrix = (a.N + COLS - 1) / COLS;  // dw: column tiles of the second matrix lie behind those of the first
+    struct Tile {
+        Segment s;
+        int row0, n0, matrix, nk;  // first row (of the segment's; dw: of the matrix) and column, stages
+    };
+    auto tile_at = [&](int t) __attribute__((always_inline)) {
+        Tile w;
+        int r, c;
+        if (DW) {
+            const int per = a.mt * a.nt;
+            w.s.e = t / per, w.s.block = 0;
+            tile_in_groups(t - w.s.e * per, a.mt, a.nt, &r, &c);
+            w.s.begin = uniform(tables->begin[w.s.e]), w.s.used = w.s.extent = uniform(tables->used[w.s.e]);
+            w.row0 = r * T::BM;
+            w.nk = (w.s.used + STEPS - 1) / STEPS;
+        } else {
+            tile_in_groups(t, row_blocks, a.nt, &r, &c);
+            const int e = last_up_to(tables->first, a.E + 1, r);
+            w.s.e = e, w.s.block = r - uniform(tables->first[e]);
+            w.s.begin = uniform(a.capacity ? e * a.capacity : tables->begin[e]);
+            w.s.used = e < a.E ? uniform(tables->used[e]) : 0;
+            w.s.extent = a.capacity ? a.capacity : e < a.E ? w.s.used : a.rows - w.s.begin;
+            w.row0 = w.s.block * T::BM;
+            w.nk = w.row0 >= w.s.used ? 0 : OP == kFfnDx ? 2 * half : half;
+        }
+        w.matrix = DW ? c / per_matrix : 0;
+        w.n0 = (c - w.matrix * per_matrix) * COLS;
+        return w;
+    };
+
+    // ---- loads.  A lane's places in the operands; they go on from stage to stage.
+    const char *ap[OA::PER_WAVE], *bp[OB::PER_WAVE];
+    const size_t lda = (size_t)a.lda * SZ, ldb = (size_t)a.ldb * SZ;
+    const size_t a_step = AK ? T::KB : STEPS * lda, b_step = BK ? T::KB : STEPS * ldb;
+    const u32 lds = lds_offset(stages);
+    int next, nk, used;  // the stage to load; stages and rows of the tile that is loaded
+    u32 to;              // where it goes
+    // before a stage's loads: on to the second pair of operands; rows past the expert's last one are that one again
+    auto begin_stage = [&]() __attribute__((always_inline)) {
+        if (OP == kFfnDx && next == half) {
+            const long long da = (const char *)a.A1 - (const char *)a.A0 - (long long)half * T::KB, db = (const char *)a.B1 - (const char *)a.B0 - (long long)half * T::KB;
+#pragma unroll
+            for (int i = 0; i < OA::PER_WAVE; ++i) ap[i] += da;
+#pragma unroll
+            for (int i = 0; i < OB::PER_WAVE; ++i) bp[i] += db;
+        }
+        if (OP == kFfnDw && next == nk - 1) {
+            const int left = used - 1 - next * STEPS;
+#pragma unroll
+            for (int i = 0; i < OA::PER_WAVE; ++i) ap[i] -= (size_t)max(OA::row_of(OA::instr(wave, i), lane) - left, 0) * lda;
+#pragma unroll
+            for (int i = 0; i < OB::PER_WAVE; ++i) bp[i] -= (size_t)max(OB::row_of(OB::instr(wave, i), lane) - left, 0) * ldb;
+        }
+    };
+    auto load_one = [&](int i) __attribute__((always_inline)) {
+        if (i < OA::PER_WAVE) {
+            load_to_lds(ap[i], to + OA::instr(wave, i) * 1024);
+            ap[i] += a_step;
+        } else {
+            const int j = i - OA::PER_WAVE;
+            load_to_lds(bp[j], to + OA::BYTES + OB::instr(wave, j) * 1024);
+            bp[j] += b_step;
+        }
+    };
+    auto end_stage = [&]() __attribute__((always_inline)) {
+        ++next;
+        to += T::STAGE;
+        if (to == lds + T::NS * T::STAGE) to = lds;
+    };
+    auto load_stage = [&]() __attribute__((always_inline)) {
+        begin_stage();
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) load_one(i);
+        end_stage();
+    };
+    // The first stages of a tile: nobody may be reading the stages any more.
+    auto start = [&](const Tile &w) __attribute__((always_inline)) {
+        nk = w.nk, used = w.s.used, next = 0, to = lds;
+        if (!nk) return;
+        const char *A = (const char *)a.A0, *B = (const char *)(DW && w.matrix ? a.B1 : a.B0);
 #pragma unroll
         for (int i = 0; i < OA::PER_WAVE; ++i) {
             const int in = OA::instr(wave, i), r = OA::row_of(in, lane), c = OA::piece_of(in, lane);
             if constexpr (AK) {
-                ap[i] = A + (size_t)(s.begin + min(row0 + r, s.used - 1)) * lda + c * 16;
+                ap[i] = A + (size_t)(w.s.begin + min(w.row0 + r, used - 1)) * lda + c * 16;
             } else {
-                const int m = row0 + c * PIECE;
-                ap[i] = A + (size_t)(s.begin + r) * lda + (size_t)(m < a.M ? m : 0) * SZ;
+                const int m = w.row0 + c * PIECE;
+                ap[i] = A + (size_t)(w.s.begin + r) * lda + (size_t)(m < a.M ? m : 0) * SZ;
             }
         }
 #pragma unroll
         for (int i = 0; i < OB::PER_WAVE; ++i) {
             const int in = OB::instr(wave, i), r = OB::row_of(in, lane), c = OB::piece_of(in, lane);
             if constexpr (BK) {
-                bp[i] = B + (size_t)s.e * a.eb * SZ + (size_t)min(n0 + r, a.N - 1) * ldb + c * 16;
+                bp[i] = B + (size_t)w.s.e * a.eb * SZ + (size_t)min(w.n0 + r, a.N - 1) * ldb + c * 16;
             } else {
                 int n = c * PIECE;
                 const char *from = B;
                 if (GATED && n >= COLS) from = (const char *)a.B1, n -= COLS;
-                n += n0;
-                const size_t first = OP == kFfnDw ? (size_t)s.begin * ldb : (size_t)s.e * a.eb * SZ;
+                n += w.n0;
+                const size_t first = DW ? (size_t)w.s.begin * ldb : (size_t)w.s.e * a.eb * SZ;
                 bp[i] = from + first + (size_t)r * ldb + (size_t)(n < a.N ? n : 0) * SZ;
             }
         }
-        const size_t a_step = AK ? 64 : STEPS * lda, b_step = BK ? 64 : STEPS * ldb;
-        const u32 lds = lds_offset(stages);
-        int next = 0, next_buf = 0;  // the stage to load, and where
-        auto load_stage = [&]() {
-            const u32 to = lds + next_buf * T::STAGE;
-            if (OP == kFfnDx && next == half) {  // on to the second pair
-                const long long da = (const char *)a.A1 - (const char *)a.A0 - (long long)half * 64, db = (const char *)a.B1 - (const char *)a.B0 - (long long)half * 64;
-#pragma unroll
-                for (int i = 0; i < OA::PER_WAVE; ++i) ap[i] += da;
-#pragma unroll
-                for (int i = 0; i < OB::PER_WAVE; ++i) bp[i] += db;
-            }
-            const int left = OP == kFfnDw ? s.used - 1 - next * STEPS : STEPS;  // the last row there is
-#pragma unroll
-            for (int i = 0; i < OA::PER_WAVE; ++i) {
-                const int in = OA::instr(wave, i);
-                const char *p = ap[i];
-                if (OP == kFfnDw) p -= (size_t)max(OA::row_of(in, lane) - left, 0) * lda;
-                load_to_lds(p, to + in * 1024);
-                ap[i] += a_step;
-            }
-#pragma unroll
-            for (int i = 0; i < OB::PER_WAVE; ++i) {
-                const int in = OB::instr(wave, i);
-                const char *p = bp[i];
-                if (OP == kFfnDw) p -= (size_t)max(OB::row_of(in, lane) - left, 0) * ldb;
-                load_to_lds(p, to + OA::BYTES + in * 1024);
-                bp[i] += b_step;
-            }
-            ++next;
-            next_buf = next_buf + 1 == T::NS ? 0 : next_buf + 1;
-        };
-        int a_at[T::MB], b_at[T::NB];
-#pragma unroll
-        for (int mb = 0; mb < T::MB; ++mb) a_at[mb] = (wm * T::MB + mb) * 32;
-#pragma unroll
-        for (int nb = 0; nb < T::NB; ++nb)
-            b_at[nb] = !GATED ? (wn * T::NB + nb) * 32 : nb < T::NB / 2 ? (wn * T::NB / 2 + nb) * 32 : COLS + (wn * T::NB / 2 + nb - T::NB / 2) * 32;
+        const int ahead = min(nk, T::NS);
+        for (int i = 0; i < ahead; ++i) load_stage();
+    };
 
-        for (int i = 0; i < T::NS - 1 && i < nk; ++i) load_stage();
-        int buf = 0;
-        for (int kt = 0; kt < nk; ++kt) {
-            // stage kt has landed when no more loads are in flight than those of the stages behind it
-            const int behind = min(nk - 1 - kt, T::NS - 2);
-            if (T::NS >= 4 && behind >= 2)
-                wait_vmcnt<2 * LPS>();
-            else if (T::NS >= 3 && behind >= 1)
-                wait_vmcnt<LPS>();
-            else
-                wait_vmcnt<0>();
-            __syncthreads();  // ... and everybody has read the stage that the next load replaces
-            if (next < nk) load_stage();
-            char *stage = stages + buf * T::STAGE;
-            if (OP == kFfnDw && kt == nk - 1 && s.used % STEPS) {
-                // the steps past the expert's last row: zeros in both operands, whatever lies there
-                const int from = s.used % STEPS;
-                for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += T::THREADS) *(u32x4_t *)(stage + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
-                for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += T::THREADS)
-                    *(u32x4_t *)(stage + OA::BYTES + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
-                __syncthreads();
+    // ---- products
+    f32x16_t acc[T::MB][T::NB];
+    int a_at[T::MB], b_at[T::NB];
+#pragma unroll
+    for (int mb = 0; mb < T::MB; ++mb) a_at[mb] = (wm * T::MB + mb) * 32;
+#pragma unroll
+    for (int nb = 0; nb < T::NB; ++nb)
+        b_at[nb] = !GATED ? (wn * T::NB + nb) * 32 : nb < T::NB / 2 ? (wn * T::NB / 2 + nb) * 32 : COLS + (wn * T::NB / 2 + nb - T::NB / 2) * 32;
+
+    // Fragments are read a step ahead of the products that take them; a stage's buffer is free when everybody has read its last
+    // fragments, and the loads of the stage that goes there are dealt out over the steps that follow.
+    constexpr int KK = T::KB / 32;  // steps per stage
+    static_assert(KK % 2 == 0, "two sets of fragments in turn");
+    constexpr int LPK = (LPS + KK - 1) / KK;
+    constexpr int NREAD = T::MB * OA::READS + T::NB * OB::READS, NMUL = T::MB * T::NB, NMFMA = NMUL * (SZ == 2 ? 1 : 4);
+    struct Frags {
+        u32x4_t a[T::MB], b[T::NB];
+    };
+    Frags f0, f1;
+    auto read = [&](const char *stage, int kk, Frags &f) __attribute__((always_inline)) {
+        read_frags<OA>(stage, kk, a_at, lane, f.a);
+        read_frags<OB>(stage + OA::BYTES, kk, b_at, lane, f.b);
+    };
+    // products of `cur`, with the reads of `nxt` and, if LOADS, share `part` of a stage's loads in between
+    auto step = [&](const char *stage, int kk, Frags &nxt, const Frags &cur, auto loads, int part) __attribute__((always_inline)) {
+        constexpr bool LOADS = decltype(loads)::value;
+        read(stage, kk, nxt);
+#pragma unroll
+        for (int mb = 0; mb < T::MB; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) {
+                const int i = mb * T::NB + nb;
+                if (LOADS) {
+#pragma unroll
+                    for (int j = 0; j < LPK; ++j)
+                        if (j * NMUL / LPK == i && part * LPK + j < LPS) load_one(part * LPK + j);
+                }
+                multiply<ET>(cur.b[nb], cur.a[mb], acc[mb][nb]);
             }
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                u32x4_t fa[T::MB], fb[T::NB];
-                read_frags<OA>(stage, kk, a_at, lane, fa);
-                read_frags<OB>(stage + OA::BYTES, kk, b_at, lane, fb);
-#pragma unroll
-                for (int mb = 0; mb < T::MB; ++mb)
-#pragma unroll
-                    for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(fb[nb], fa[mb], acc[mb][nb]);
-            }
-            buf = buf + 1 == T::NS ? 0 : buf + 1;
+        for (int i = 0; i < NMFMA; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product ...
+            if (i < NREAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // ... an LDS read
         }
+        if (NREAD > NMFMA) __builtin_amdgcn_sched_group_barrier(0x100, NREAD - NMFMA, 0);
+    };
+    // stage kt has landed, and everybody has read what the next loads replace
+    auto landed = [&](int kt, int behind) __attribute__((always_inline)) {
+        static_assert(T::NS <= 4, "waits");
+        if (T::NS >= 4 && behind >= 3)
+            wait_vmcnt<3 * LPS>();
+        else if (T::NS >= 4 && behind == 2)
+            wait_vmcnt<2 * LPS>();
+        else if (T::NS >= 3 && behind == 2)
+            wait_vmcnt<2 * LPS>();
+        else if (behind == 1)
+            wait_vmcnt<LPS>();
+        else
+            wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __syncthreads();
-    }
+        if (OP == kFfnDw && kt == nk - 1 && used % STEPS) {
+            // the steps past the expert's last row: zeros in both operands, whatever lies there
+            char *stage = stages + kt % T::NS * T::STAGE;
+            const int from = used % STEPS;
+            for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += T::THREADS) *(u32x4_t *)(stage + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+            for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += T::THREADS)
+                *(u32x4_t *)(stage + OA::BYTES + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+            __syncthreads();
+        }
+    };
 
-    // Out through LDS of the wavefront's own: 32 rows x 64 columns of sums at a time (up: 32 or 64 of g, and of u), written as the
-    // matrix cores leave them and read as rows, 8 columns a lane.
-    char *out = stages + wave * T::OUT;
-    constexpr int BLOCKS = GATED ? T::NB / 2 : 2, CHUNKS = GATED ? 1 : T::NB / 2;  // blocks of columns at a time, and how often
-    constexpr int LANES = BLOCKS * 4, ROWS = 64 / LANES;
+    // ---- out.  128 bytes of 32 rows (64 columns of bf16, 32 of fp32; less where a wavefront has less) go through LDS of the wavefront's own: the
+    // matrix cores leave lane l with row l & 31, columns 8 q + 4 (l >> 5) + 0..3 of a block; memory is reached in pieces of 16 bytes.
+    constexpr int COL_BLOCKS = GATED ? T::NB / 2 : T::NB;
+    constexpr int GROUP = SZ == 2 && COL_BLOCKS % 2 == 0 ? 2 : 1;  // blocks at a time
+    constexpr int LANES = GROUP * 32 / PIECE, ROWS = 64 / LANES;  // lanes per row, rows at a time
+    char *out = smem + T::AT_OUT + wave * T::OUT;
+    typedef u32x4_t __attribute__((may_alias)) Piece16;
+    typedef __attribute__((ext_vector_type(2))) u32 u32x2_t;
+    typedef u32x2_t __attribute__((may_alias)) Piece8;
+    auto write_tile = [&](const Tile &w) __attribute__((always_inline)) {
+        const int rows = DW ? a.M : w.s.extent;
 #pragma unroll
-    for (int mb = 0; mb < T::MB; ++mb)
+        for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
-        for (int ch = 0; ch < CHUNKS; ++ch) {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int gb = 0; gb < COL_BLOCKS; gb += GROUP) {
+                __builtin_amdgcn_sched_barrier(0);  // (results of one group at a time: registers)
+                const int m0 = w.row0 + (wm * T::MB + mb) * 32, n0 = w.n0 + (wn * COL_BLOCKS + gb) * 32;
+                if (n0 >= a.N || m0 >= rows) continue;
+                const size_t first = DW ? 0 : (size_t)w.s.begin;
+                // (or the places and sums of all groups are fetched ahead into vector registers, and spilled)
+                int l = lane;
+                asm volatile("" : "+v"(l));
 #pragma unroll
-            for (int h = 0; h < (GATED ? 2 : 1); ++h)
+                for (int b = 0; b < GROUP; ++b) {
+                    asm volatile("" : "+a"(acc[mb][gb + b]));
+                    if (GATED) asm volatile("" : "+a"(acc[mb][gb + b + T::NB / 2]));
+                }
+                const int out_r = l / LANES, out_c = l % LANES * PIECE;
+                // f(row of the matrix, column, number of the piece) where there are such elements
+                auto each_piece = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x16_t &v = acc[mb][GATED ? h * (T::NB / 2) + b : ch * 2 + b];
-                        *(f32x4_t *)(out + h * T::OUT_HALF + (lane & 31) * T::OUT_ROW + (b * 32 + q * 8 + (lane >> 5) * 4) * 4) =
-                            f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    for (int i = 0; i < 32 / ROWS; ++i) {
+                        const int m = m0 + i * ROWS + out_r, n = n0 + out_c;
+                        if (n < a.N && m < rows) f(m, first + m, n, i);
                     }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int c = (lane % LANES) * 8;
-            const int n = n0 + (GATED ? wn * T::NB / 2 * 32 : (wn * T::NB + ch * 2) * 32) + c;
+                };
+                auto put = [&](auto value, void *to, long long ld) __attribute__((always_inline)) {  // value(block, register)
+                    asm volatile("" ::: "memory");
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += ROWS) {
-                const int r = r0 + lane / LANES, m = row0 + (wm * T::MB + mb) * 32 + r;
-                if (n >= a.N || m >= (OP == kFfnDw ? a.M : s.extent)) continue;
-                const bool used = OP == kFfnDw || m < s.used;
-                float v[8], w[8];
-                const float *p = (const float *)(out + r * T::OUT_ROW) + c;
+                    for (int b = 0; b < GROUP; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = used ? p[j] : 0.f;  // (an unused row has the sums of a used one)
-                const size_t row = (size_t)(s.begin + m), at = row * a.N + n;
-                if constexpr (OP == kFfnUp) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = used ? p[T::OUT_HALF / 4 + j] : 0.f;
-                    if (a.o0) {
-                        store8<ET>(a.o0, row * a.ldo + n, v);
-                        store8<ET>(a.o1, row * a.ldo + n, w);
-                    }
-                    if (a.o2) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = v[j] * sigmoid<ET>(v[j]) * w[j];
-                        store8<ET>(a.o2, at, v);
-                    }
-                } else if constexpr (OP == kFfnDh) {
-                    if (a.o2) store8<ET>(a.o2, at, v);
-                    if (a.o0) {
-                        float g[8], u[8];
-                        load8<ET>(a.g, row * a.ldg + n, g);
-                        load8<ET>(a.u, row * a.ldg + n, u);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float sg = sigmoid<ET>(g[j]);
-                            w[j] = used ? v[j] * (g[j] * sg) : 0.f;
-                            v[j] = used ? v[j] * (u[j] * (sg * (1.f + g[j] * (1.f - sg)))) : 0.f;
+                        for (int q = 0; q < 4; ++q) {
+                            char *p = out + (l & 31) * T::OUT_ROW + (b * 32 + q * 8 + (l >> 5) * 4) * SZ;
+                            const float v[4] = {value(b, 4 * q), value(b, 4 * q + 1), value(b, 4 * q + 2), value(b, 4 * q + 3)};
+                            if constexpr (SZ == 2)
+                                *(Piece8 *)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                            else
+                                *(Piece16 *)p = Piece<float>::pack(v);
                         }
-                        store8<ET>(a.o0, row * a.ldo + n, v);
-                        store8<ET>(a.o1, row * a.ldo + n, w);
+                    asm volatile("" ::: "memory");
+                    each_piece([&](int m, size_t row, int n, int i) __attribute__((always_inline)) {
+                        u32x4_t v = *(const Piece16 *)(out + (i * ROWS + out_r) * T::OUT_ROW + out_c * SZ);
+                        if (!DW && m >= w.s.used) v = u32x4_t{0, 0, 0, 0};  // (an unused row has the sums of a used one)
+                        *(Piece16 *)((ET *)to + row * ld + n) = v;
+                    });
+                };
+                if constexpr (OP == kFfnUp) {
+                    auto g = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; };
+                    auto u = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b + T::NB / 2][i]; };
+                    if (a.o0) put(g, a.o0, a.ldo), put(u, a.o1, a.ldo);
+                    if (a.o2) put([&](int b, int i) __attribute__((always_inline)) { return g(b, i) * sigmoid<ET>(g(b, i)) * u(b, i); }, a.o2, a.N);
+                } else if constexpr (OP == kFfnDh) {
+                    auto dh = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; };
+                    if (a.o2) put(dh, a.o2, a.N);
+                    if (!a.o0) continue;
+                    u32x4_t gv[32 / ROWS] = {}, uv[32 / ROWS] = {};
+                    each_piece([&](int, size_t row, int n, int i) __attribute__((always_inline)) {
+                        gv[i] = *(const Piece16 *)((const ET *)a.g + row * a.ldg + n), uv[i] = *(const Piece16 *)((const ET *)a.u + row * a.ldg + n);
+                    });
+                    float s[GROUP * 16], u[GROUP * 16];
+                    auto take = [&](const u32x4_t (&v)[32 / ROWS], float *x) __attribute__((always_inline)) {  // pieces to where the sums are
+                        asm volatile("" ::: "memory");
+#pragma unroll
+                        for (int i = 0; i < 32 / ROWS; ++i) *(Piece16 *)(out + (i * ROWS + out_r) * T::OUT_ROW + out_c * SZ) = v[i];
+                        asm volatile("" ::: "memory");
+#pragma unroll
+                        for (int b = 0; b < GROUP; ++b)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const char *p = out + (l & 31) * T::OUT_ROW + (b * 32 + q * 8 + (l >> 5) * 4) * SZ;
+                                if constexpr (SZ == 2) {
+                                    const u32x2_t y = *(const Piece8 *)p;
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) x[b * 16 + 4 * q + j] = __uint_as_float(j & 1 ? y[j / 2] & 0xffff0000u : y[j / 2] << 16);
+                                } else {
+                                    Piece<float>::unpack(*(const Piece16 *)p, x + b * 16 + 4 * q);
+                                }
+                            }
+                    };
+                    take(gv, s);
+                    take(uv, u);
+#pragma unroll
+                    for (int i = 0; i < GROUP * 16; ++i) {
+                        const float g = s[i], sg = sigmoid<ET>(g);
+                        s[i] = g * sg;
+                        u[i] = u[i] * (sg * (1.f + g * (1.f - sg)));
                     }
-                } else if constexpr (OP == kFfnDw) {
-                    store8<ET>(matrix ? a.o1 : a.o0, (size_t)s.e * a.eo + (size_t)m * a.ldo + n, v);
+                    put([&](int b, int i) __attribute__((always_inline)) { return dh(b, i) * u[b * 16 + i]; }, a.o0, a.ldo);
+                    put([&](int b, int i) __attribute__((always_inline)) { return dh(b, i) * s[b * 16 + i]; }, a.o1, a.ldo);
+                } else if constexpr (DW) {
+                    put([&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; }, (ET *)(w.matrix ? a.o1 : a.o0) + (size_t)w.s.e * a.eo, a.ldo);
                 } else {
-                    store8<ET>(a.o0, at, v);
+                    put([&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; }, a.o0, a.N);
                 }
             }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // The next tile's first stages are on their way while this one's results go out.
+    Tile now = tile_at(range.next);
+    start(now);
+    while (true) {
+#pragma unroll
+        for (int mb = 0; mb < T::MB; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[mb][nb][v] = 0.f;
+        if (nk) {
+            landed(0, min(nk, T::NS) - 1);
+            char *stage = stages;
+            auto first_steps = [&](auto loads) __attribute__((always_inline)) {  // of a stage: all but the last
+#pragma unroll
+                for (int kk = 0; kk + 1 < KK; ++kk) {
+                    if (kk & 1)
+                        step(stage, kk + 1, f0, f1, loads, kk + 1);
+                    else
+                        step(stage, kk + 1, f1, f0, loads, kk + 1);
+                }
+            };
+            auto on = [&]() __attribute__((always_inline)) {
+                stage += T::STAGE;
+                if (stage == stages + T::NS * T::STAGE) stage = stages;
+            };
+            read(stage, 0, f0);
+            first_steps(std::false_type{});
+            int kt = 1;
+            for (; kt <= nk - T::NS; ++kt) {  // (T::NS - 2 stages are in flight behind this one)
+                landed(kt, T::NS - 2);
+                on();
+                begin_stage();
+                step(stage, 0, f0, f1, std::true_type{}, 0);
+                first_steps(std::true_type{});
+                end_stage();
+            }
+            for (; kt < nk; ++kt) {
+                landed(kt, min(nk - 1 - kt, T::NS - 2));
+                on();
+                step(stage, 0, f0, f1, std::false_type{}, 0);
+                first_steps(std::false_type{});
+            }
+#pragma unroll
+            for (int mb = 0; mb < T::MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(f1.b[nb], f1.a[mb], acc[mb][nb]);
+            __syncthreads();
         }
+        range.next += range.step;
+        const bool more = range.next < range.to;
+        const Tile done = now;
+        if (more) now = tile_at(range.next), start(now);
+        write_tile(done);
+        if (!more) break;
+    }
 }
 
 }  // namespace moe

@@ -11,13 +11,27 @@ static int rows_of(const moe_problem_t *p) { return p->capacity > 0 ? p->E * p->
 static int elem_bytes(const moe_problem_t *p) { return p->dtype == MOE_DT_F32 ? 4 : 2; }
 static bool bad_stride(const moe_problem_t *p, int64_t ld, int cols) { return ld < cols || ld * elem_bytes(p) % 16 != 0; }
 
+// Of the current device, asked of the runtime once.
+static int compute_units(int *n) {
+    constexpr int kDevices = 64;
+    static int known[kDevices];  // (whoever writes, writes the same)
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return MOE_ERR_HIP;
+    int cus = device < kDevices ? __atomic_load_n(&known[device], __ATOMIC_RELAXED) : 0;
+    if (!cus) {
+        if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) return MOE_ERR_HIP;
+        if (device < kDevices) __atomic_store_n(&known[device], cus, __ATOMIC_RELAXED);
+    }
+    *n = (cus + kTileQueues - 1) / kTileQueues * kTileQueues;
+    return MOE_OK;
+}
+
 template <class T, FfnOp OP>
 static int launch(FfnArgs a, hipStream_t st) {
     constexpr int COLS = OP == kFfnUp ? T::BN / 2 : T::BN;
     a.nt = (a.N + COLS - 1) / COLS * (OP == kFfnDw && a.o1 ? 2 : 1);
     a.mt = (a.M + T::BM - 1) / T::BM;
-    // as many workgroups as there can be tiles, whatever the counts are: a row block per BM rows and one more per expert (ragged: and for
-    // the rows behind the last one)
+    // row blocks, at most: one per BM rows and one more per expert (ragged: and for the rows behind the last one)
     size_t blocks;
     if (OP == kFfnDw)
         blocks = (size_t)a.E * a.mt;
@@ -25,28 +39,39 @@ static int launch(FfnArgs a, hipStream_t st) {
         blocks = (size_t)a.E * ((a.capacity + T::BM - 1) / T::BM);
     else
         blocks = (size_t)a.rows / T::BM + (size_t)(a.E < a.rows ? a.E : a.rows) + 1;
-    const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues;
-    if (tiles * T::THREADS >= (size_t)1 << 32) return MOE_ERR_UNSUPPORTED;
+    if (blocks * a.nt >= (size_t)1 << 30) return MOE_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
+    int cus = 0;
+    if (const int rc = compute_units(&cus)) return rc;
     if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
-    hipLaunchKernelGGL((k_ffn<T, OP>), dim3((unsigned)tiles), dim3(T::THREADS), T::SMEM, st, a);
+    const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * (160 * 1024 / T::SMEM);
+    hipLaunchKernelGGL((k_ffn<T, OP>), dim3((unsigned)(tiles < room ? tiles : room)), dim3(T::THREADS), T::SMEM, st, a);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
 template <typename ET, FfnOp OP>
 static int pick(const FfnArgs &a, int slots, hipStream_t st) {
     if constexpr (sizeof(ET) == 4) {
-        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 2, 2, 2, 4>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 4>, OP>(a, st);
+        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 2, 2, 2, 64, 4>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 64, 4>, OP>(a, st);
     } else {
-        if (slots / a.E > 160) return launch<FfnTile<ET, 2, 4, 4, 2, 4>, OP>(a, st);
-        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 4, 2, 2, 3>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 4>, OP>(a, st);
+#ifndef V256
+#define V256 4, 4, 2, 2, 64, 4
+#endif
+#ifndef V128
+#define V128 2, 4, 2, 2, 64, 4
+#endif
+#ifndef V32
+#define V32 1, 2, 1, 4, 128, 3
+#endif
+        if (slots / a.E > 160) return launch<FfnTile<ET, V256>, OP>(a, st);
+        return slots / a.E > 48 ? launch<FfnTile<ET, V128>, OP>(a, st) : launch<FfnTile<ET, V32>, OP>(a, st);
     }
 }
 template <typename ET>
 static int pick_dw(const FfnArgs &a, hipStream_t st) {
     if constexpr (sizeof(ET) == 4)
-        return launch<FfnTile<ET, 2, 2, 2, 2, 4>, kFfnDw>(a, st);
+        return launch<FfnTile<ET, 2, 2, 2, 2, 64, 4>, kFfnDw>(a, st);
     else
-        return launch<FfnTile<ET, 2, 4, 4, 2, 4>, kFfnDw>(a, st);
+        return launch<FfnTile<ET, V256>, kFfnDw>(a, st);
 }
 template <FfnOp OP>
 static int pick(const moe_problem_t *p, const FfnArgs &a, void *stream) {
