@@ -32,6 +32,7 @@ struct FfnArgs {
     const void *A0, *A1, *B0, *B1;
     const void *g, *u;  // dh: the activation's inputs
     void *o0, *o1, *o2;
+    const struct FfnPlan *plan;  // of k_ffn_plan, NULL: every workgroup makes its own tables and takes every n-th tile
 };
 
 constexpr int kDwStart = 96;  // rows of reduction that the start and end of a tile of dw cost as much as
@@ -56,7 +57,7 @@ struct Operand {
         return R >= 128 ? c ^ ((row & 3) << 2) : c ^ (((row >> 1) & 1) << 2);
     }
     // (where there are fewer instructions than wavefronts the upper ones repeat the lower ones': the same bytes to the same place)
-    static __device__ __forceinline__ int instr(int wave, int i) { return (wave * PER_WAVE + i) % INSTR; }
+    static __device__ __forceinline__ int instr(int wave, int i) { return (i * WAVES + wave) % INSTR; }
     static __device__ __forceinline__ int row_of(int instr, int lane) { return instr * ROWS_PER_INSTR + lane / PIECES; }
     static __device__ __forceinline__ int piece_of(int instr, int lane) { return place(row_of(instr, lane), lane % PIECES); }
 };
@@ -70,12 +71,17 @@ __device__ __forceinline__ void load_to_lds(const char *src, u32 lds) {
 struct Segment {
     int e, begin, used, extent, block;
 };
-// Where every expert's rows lie, as a workgroup finds out once.
+// Where every expert's rows lie, and which tiles each XCD takes.
 struct FfnTables {
-    u64 sum[16];
     int begin[kMaxExperts + 1], used[kMaxExperts];  // begin[E]: behind the last one's (ragged)
     int first[kMaxExperts + 1];  // first row block of an expert, of the rows of nobody behind the last (ragged); dw: rows before, and kDwStart for each expert
-    int n_tiles;
+    int edge[kTileQueues + 1];   // tiles [edge[x], edge[x + 1]) are XCD x's
+    int next;                    // in a workgroup's copy: the tile it takes next
+    u64 sum[8];                  // scratch
+};
+struct FfnPlan {
+    FfnTables tables;
+    mutable Counter taken[kTileQueues];  // tiles handed out of an XCD's list, beyond the first ones
 };
 
 // MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts, stages of KB bytes of the reduction, NS of them.
@@ -84,15 +90,12 @@ struct FfnTile {
     typedef ET_ ET;
     static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KB = KB_, NS = NS_, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * KB;
-    // a block of a wavefront's sums on its way out, 32 rows x 32 columns of fp32
-    static constexpr int OUT_ROW = 32 * 4 + 16, OUT = 32 * OUT_ROW;
-    static constexpr int AT_OUT = NS * STAGE, AT_TABLES = AT_OUT + WAVES * OUT;
+    static constexpr int AT_TABLES = NS * STAGE;
     static constexpr int SMEM = AT_TABLES + (int)sizeof(FfnTables);
     static_assert(SMEM <= 160 * 1024, "LDS");
 };
 
-template <int WAVES>
-__device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  // inclusive
+__device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  // inclusive, kThreads threads
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -103,7 +106,7 @@ __device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  //
     __syncthreads();
     u64 before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < kThreads / 64; ++w) {
         if (w < wave) before += lds[w];
         all += lds[w];
     }
@@ -111,28 +114,6 @@ __device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  //
     return v + before;
 }
 
-// The tables, by all threads.  Ragged: thread i has expert i.
-template <class T, bool DW>
-__device__ __forceinline__ void make_tables(const FfnArgs &a, FfnTables *t) {
-    const int tid = threadIdx.x;
-    const int n = tid < a.E ? max(a.counts[tid], 0) : 0;
-    int begin, used, blocks;
-    if (a.capacity) {
-        begin = tid * a.capacity, used = min(n, a.capacity), blocks = (a.capacity + T::BM - 1) / T::BM;
-    } else {
-        u64 all;
-        const u64 end = scan_workgroup<T::WAVES>((u64)min(n, a.rows), t->sum, &all);
-        begin = (int)min(end - min(n, a.rows), (u64)a.rows), used = (int)min(end, (u64)a.rows) - begin, blocks = (used + T::BM - 1) / T::BM;
-        if (tid == 0) t->begin[a.E] = (int)min(all, (u64)a.rows);
-    }
-    if (DW) blocks = used + kDwStart;
-    if (tid >= a.E) blocks = 0;
-    u64 all;
-    const int to = (int)scan_workgroup<T::WAVES>((u64)blocks, t->sum + 8, &all);
-    if (tid < a.E) t->begin[tid] = begin, t->used[tid] = used, t->first[tid] = to - blocks;
-    if (tid == 0) t->first[a.E] = (int)all;
-    __syncthreads();
-}
 // The last of the E + 1 ascending numbers that is `v` or less (the first one is).
 __device__ __forceinline__ int last_up_to(const int *list, int n, int v) {
     int found = 0;
@@ -148,33 +129,69 @@ __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r
     *r = first + in % n, *c = in / n;
 }
 
-// Workgroups go round the eight XCDs; each XCD takes a stretch of the tiles, whose neighbours read the same operands, from its own L2: tiles
-// [from, to), workgroup number `id` / 8 of the XCD every `step`-th.
-struct TileRange {
-    int next, to, step;
-};
+// The tables (in LDS), by kThreads threads; thread i has expert i.  Workgroups go round the eight XCDs, and each XCD takes a stretch of the tiles,
+// whose neighbours read the same operands, from its own L2.
 template <bool DW>
-__device__ __forceinline__ TileRange tiles_of(const FfnArgs &a, const FfnTables *t, int row_blocks) {
-    const int x = blockIdx.x % kTileQueues;
-    int edge[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+__device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables *t) {
+    const int tid = threadIdx.x;
+    static_assert(kThreads >= kMaxExperts, "a thread per expert");
+    const int n = tid < a.E ? min(max(a.counts[tid], 0), a.rows) : 0;
+    int begin, used, blocks;
+    u64 all;
+    if (a.capacity) {
+        begin = tid * a.capacity, used = min(n, a.capacity), blocks = (a.capacity + bm - 1) / bm;
+    } else {
+        const u64 end = scan_workgroup((u64)n, t->sum, &all);
+        begin = (int)min(end - n, (u64)a.rows), used = (int)min(end, (u64)a.rows) - begin, blocks = (used + bm - 1) / bm;
+        if (tid == 0) t->begin[a.E] = (int)min(all, (u64)a.rows);
+    }
+    if (DW) blocks = used + kDwStart;
+    if (tid >= a.E) blocks = 0;
+    const int to = (int)scan_workgroup((u64)blocks, t->sum + 4, &all);
+    if (tid < a.E) t->begin[tid] = begin, t->used[tid] = used, t->first[tid] = to - blocks;
+    if (tid == 0) t->first[a.E] = (int)all;
+    __syncthreads();
+    const int total = (int)all;
+    if (tid <= kTileQueues) {
         if (DW) {
             // stretches of about the same work: a tile is worth its expert's rows and kDwStart
-            const u64 at = (u64)(x + i) * (u32)t->first[a.E];
-            const int e = min(last_up_to(t->first, a.E + 1, (int)(at / kTileQueues)), a.E - 1), per = a.mt * a.nt;
-            edge[i] = x + i == kTileQueues ? a.E * per : e * per + (int)((at - (u64)kTileQueues * t->first[e]) * per / (u64)(kTileQueues * (t->used[e] + kDwStart)));
+            const int per = a.mt * a.nt;
+            const u64 at = (u64)tid * (u32)total;
+            int e = 0;
+            for (int step = kMaxExperts / 2; step; step >>= 1)
+                if (e + step < a.E && t->first[e + step] <= (int)(at / kTileQueues)) e += step;
+            t->edge[tid] = tid == kTileQueues ? a.E * per : e * per + (int)((at - (u64)kTileQueues * t->first[e]) * per / (u64)(kTileQueues * (t->used[e] + kDwStart)));
         } else {
-            edge[i] = (int)((i64)row_blocks * a.nt * (x + i) / kTileQueues);
+            const int row_blocks = total + (a.capacity ? 0 : (a.rows - t->begin[a.E] + bm - 1) / bm);
+            t->edge[tid] = (int)((i64)row_blocks * a.nt * tid / kTileQueues);
         }
     }
-    return TileRange{edge[0] + (int)(blockIdx.x / kTileQueues), edge[1], (int)(gridDim.x / kTileQueues)};
+    __syncthreads();
+}
+
+// One workgroup makes the tables for the launch or two that follow.
+struct FfnPlanArgs {
+    FfnArgs rows, dw;  // the launches'
+    FfnPlan *rows_plan, *dw_plan;  // NULL: there is none
+    int bm;
+};
+__global__ __launch_bounds__(kThreads) void k_ffn_plan(FfnPlanArgs a) {
+    __shared__ FfnTables t;
+    const int tid = threadIdx.x;
+    auto out = [&](FfnPlan *p) {
+        for (int i = tid; i < (int)(sizeof(FfnTables) / 4); i += kThreads) ((u32 *)&p->tables)[i] = ((const u32 *)&t)[i];
+        if (tid < kTileQueues) p->taken[tid].v = 0;
+        __syncthreads();
+    };
+    if (a.rows_plan) make_tables<false>(a.rows, a.bm, &t), out(a.rows_plan);
+    if (a.dw_plan) make_tables<true>(a.dw, 1, &t), out(a.dw_plan);
 }
 
 // The fragments of N blocks of an operand for step `kk` (32 bytes of the reduction) of a stage: lane l has index l & 31 of a block and the
 // steps of its half, l >> 5: 8 of bf16, 4 of fp32.
-template <class O, int N>
-__device__ __forceinline__ void read_frags(const char *stage, int kk, const int (&at)[N], int lane, u32x4_t (&f)[N]) {
+template <class O, int N, int M>
+__device__ __forceinline__ void read_frags(const char *stage, int kk, const int (&at)[M], int lane, u32x4_t (&f)[N]) {
+    static_assert(N <= M, "blocks");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if constexpr (O::KC) {
@@ -213,17 +230,45 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     typedef Operand<ET, T::BN, BK, T::KB, T::WAVES> OB;
     constexpr int LPS = OA::PER_WAVE + OB::PER_WAVE, SZ = sizeof(ET), STEPS = OA::STEPS, PIECE = 16 / SZ;
     constexpr int COLS = GATED ? T::BN / 2 : T::BN;  // columns of a matrix per tile
-    static_assert(T::THREADS >= kMaxExperts, "a thread per expert");
     static_assert(!GATED || T::NB % 2 == 0, "g and u of the same columns");
     extern __shared__ __align__(128) char smem[];
     char *stages = smem;
-    const FfnTables *tables = (const FfnTables *)(smem + T::AT_TABLES);
-    make_tables<T, DW>(a, (FfnTables *)tables);
+    FfnTables *tables = (FfnTables *)(smem + T::AT_TABLES);
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
-    const int used_blocks = tables->first[a.E];
-    const int row_blocks = uniform(DW || a.capacity ? used_blocks : used_blocks + (a.rows - tables->begin[a.E] + T::BM - 1) / T::BM);
-    TileRange range = tiles_of<DW>(a, tables, row_blocks);
-    if (range.next >= range.to) return;
+    static_assert(T::THREADS == kThreads, "four wavefronts");
+    if (a.plan) {
+        for (int i = tid; i < (int)(sizeof(FfnTables) / 4); i += kThreads) ((u32 *)tables)[i] = ((const u32 *)&a.plan->tables)[i];
+        __syncthreads();
+    } else {
+        make_tables<DW>(a, T::BM, tables);
+    }
+    const int row_blocks = uniform(tables->edge[kTileQueues]) / a.nt;  // (dw: of tiles)
+    // The tile after this one.  Where there is a plan, tiles are handed out as workgroups come for them, first of the own XCD's list, then of
+    // the others': experts' last row blocks, and dw's experts, differ in what they take.
+    int list = blockIdx.x % kTileQueues;
+    const int mine = blockIdx.x / kTileQueues, per_list = gridDim.x / kTileQueues;
+    int taken = 0;  // thread 0: what it was given of `list`
+    auto ask = [&]() __attribute__((always_inline)) {
+        if (a.plan && tid == 0) taken = (int)atomicAdd(&a.plan->taken[list].v, 1u);
+    };
+    auto answer = [&]() __attribute__((always_inline)) {  // thread 0; the others read it behind a barrier
+        if (!a.plan || tid) return;
+        int t = tables->edge[list] + per_list + taken;
+        for (int tries = 1; t >= tables->edge[list + 1] && tries < kTileQueues; ++tries) {
+            list = (list + 1) % kTileQueues;
+            t = tables->edge[list] + per_list + (int)atomicAdd(&a.plan->taken[list].v, 1u);
+        }
+        tables->next = t < tables->edge[list + 1] ? t : -1;
+    };
+    int tile = uniform(tables->edge[list]) + mine;
+    if (tile >= uniform(tables->edge[list + 1])) {
+        if (!a.plan) return;
+        ask();
+        answer();
+        __syncthreads();
+        tile = uniform(tables->next);
+        if (tile < 0) return;
+    }
 
     const int half = a.K / STEPS;  // stages of a pair of operands
     const int per_matrix = (a.N + COLS - 1) / COLS;  // dw: column tiles of the second matrix lie behind those of the first
@@ -256,12 +301,17 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
         return w;
     };
 
+    // Row blocks that are not full: loops of their own for a quarter, a half and three quarters of the rows.  (A wavefront has all rows then.)
+    constexpr bool SHORT = !DW && T::WM == 1 && T::MB % 4 == 0;
+    auto loads_of_a = [](int live) __attribute__((always_inline)) { return (OA::INSTR * live / T::MB + T::WAVES - 1) / T::WAVES; };
+
     // ---- loads.  A lane's places in the operands; they go on from stage to stage.
     const char *ap[OA::PER_WAVE], *bp[OB::PER_WAVE];
     const size_t lda = (size_t)a.lda * SZ, ldb = (size_t)a.ldb * SZ;
     const size_t a_step = AK ? T::KB : STEPS * lda, b_step = BK ? T::KB : STEPS * ldb;
     const u32 lds = lds_offset(stages);
     int next, nk, used;  // the stage to load; stages and rows of the tile that is loaded
+    int live, a_loads;   // blocks of 32 rows it has (LIVES), loads of A per wavefront
     u32 to;              // where it goes
     // before a stage's loads: on to the second pair of operands; rows past the expert's last one are that one again
     auto begin_stage = [&]() __attribute__((always_inline)) {
@@ -298,13 +348,20 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     auto load_stage = [&]() __attribute__((always_inline)) {
         begin_stage();
 #pragma unroll
-        for (int i = 0; i < LPS; ++i) load_one(i);
+        for (int i = 0; i < LPS; ++i)
+            if (i >= a_loads && i < OA::PER_WAVE)
+                continue;
+            else
+                load_one(i);
         end_stage();
     };
     // The first stages of a tile: nobody may be reading the stages any more.
     auto start = [&](const Tile &w) __attribute__((always_inline)) {
         nk = w.nk, used = w.s.used, next = 0, to = lds;
         if (!nk) return;
+        const int rows = used - w.row0;
+        live = !SHORT || rows > T::BM / 4 * 3 ? T::MB : rows > T::BM / 2 ? T::MB / 4 * 3 : rows > T::BM / 4 ? T::MB / 2 : T::MB / 4;
+        a_loads = loads_of_a(live);
         const char *A = (const char *)a.A0, *B = (const char *)(DW && w.matrix ? a.B1 : a.B0);
 #pragma unroll
         for (int i = 0; i < OA::PER_WAVE; ++i) {
@@ -347,175 +404,209 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     // fragments, and the loads of the stage that goes there are dealt out over the steps that follow.
     constexpr int KK = T::KB / 32;  // steps per stage
     static_assert(KK % 2 == 0, "two sets of fragments in turn");
-    constexpr int LPK = (LPS + KK - 1) / KK;
-    constexpr int NREAD = T::MB * OA::READS + T::NB * OB::READS, NMUL = T::MB * T::NB, NMFMA = NMUL * (SZ == 2 ? 1 : 4);
-    struct Frags {
-        u32x4_t a[T::MB], b[T::NB];
-    };
-    Frags f0, f1;
-    auto read = [&](const char *stage, int kk, Frags &f) __attribute__((always_inline)) {
-        read_frags<OA>(stage, kk, a_at, lane, f.a);
-        read_frags<OB>(stage + OA::BYTES, kk, b_at, lane, f.b);
-    };
-    // products of `cur`, with the reads of `nxt` and, if LOADS, share `part` of a stage's loads in between
-    auto step = [&](const char *stage, int kk, Frags &nxt, const Frags &cur, auto loads, int part) __attribute__((always_inline)) {
-        constexpr bool LOADS = decltype(loads)::value;
-        read(stage, kk, nxt);
+    auto products = [&](auto blocks) __attribute__((always_inline)) {
+        constexpr int LIVE = decltype(blocks)::value;
+        constexpr int AL = (OA::INSTR * LIVE / T::MB + T::WAVES - 1) / T::WAVES, LPS = AL + OB::PER_WAVE;  // loads per wavefront and stage
+        constexpr int LPK = (LPS + KK - 1) / KK;
+        constexpr int NREAD = LIVE * OA::READS + T::NB * OB::READS, NMUL = LIVE * T::NB, NMFMA = NMUL * (SZ == 2 ? 1 : 4);
+        struct Frags {
+            u32x4_t a[LIVE], b[T::NB];
+        };
+        Frags f0, f1;
+        auto read = [&](const char *stage, int kk, Frags &f) __attribute__((always_inline)) {
+            read_frags<OA>(stage, kk, a_at, lane, f.a);
+            read_frags<OB>(stage + OA::BYTES, kk, b_at, lane, f.b);
+        };
+        // products of `cur`, with the reads of `nxt` and, if LOADS, share `part` of a stage's loads in between
+        auto step = [&](const char *stage, int kk, Frags &nxt, const Frags &cur, auto loads, int part) __attribute__((always_inline)) {
+            constexpr bool LOADS = decltype(loads)::value;
+            read(stage, kk, nxt);
 #pragma unroll
-        for (int mb = 0; mb < T::MB; ++mb)
+            for (int mb = 0; mb < LIVE; ++mb)
 #pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) {
-                const int i = mb * T::NB + nb;
-                if (LOADS) {
+                for (int nb = 0; nb < T::NB; ++nb) {
+                    const int i = mb * T::NB + nb;
+                    if (LOADS) {
 #pragma unroll
-                    for (int j = 0; j < LPK; ++j)
-                        if (j * NMUL / LPK == i && part * LPK + j < LPS) load_one(part * LPK + j);
+                        for (int j = 0; j < LPK; ++j)
+                            if (j * NMUL / LPK == i && part * LPK + j < LPS) load_one(part * LPK + j < AL ? part * LPK + j : part * LPK + j - AL + OA::PER_WAVE);
+                    }
+                    multiply<ET>(cur.b[nb], cur.a[mb], acc[mb][nb]);
                 }
-                multiply<ET>(cur.b[nb], cur.a[mb], acc[mb][nb]);
-            }
 #pragma unroll
-        for (int i = 0; i < NMFMA; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product ...
-            if (i < NREAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // ... an LDS read
-        }
-        if (NREAD > NMFMA) __builtin_amdgcn_sched_group_barrier(0x100, NREAD - NMFMA, 0);
-    };
-    // stage kt has landed, and everybody has read what the next loads replace
-    auto landed = [&](int kt, int behind) __attribute__((always_inline)) {
-        static_assert(T::NS <= 4, "waits");
-        if (T::NS >= 4 && behind >= 3)
-            wait_vmcnt<3 * LPS>();
-        else if (T::NS >= 4 && behind == 2)
-            wait_vmcnt<2 * LPS>();
-        else if (T::NS >= 3 && behind == 2)
-            wait_vmcnt<2 * LPS>();
-        else if (behind == 1)
-            wait_vmcnt<LPS>();
-        else
-            wait_vmcnt<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (OP == kFfnDw && kt == nk - 1 && used % STEPS) {
-            // the steps past the expert's last row: zeros in both operands, whatever lies there
-            char *stage = stages + kt % T::NS * T::STAGE;
-            const int from = used % STEPS;
-            for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += T::THREADS) *(u32x4_t *)(stage + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
-            for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += T::THREADS)
-                *(u32x4_t *)(stage + OA::BYTES + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+            for (int i = 0; i < NMFMA; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product ...
+                if (i < NREAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // ... an LDS read
+            }
+            if (NREAD > NMFMA) __builtin_amdgcn_sched_group_barrier(0x100, NREAD - NMFMA, 0);
+        };
+        // stage kt has landed, and everybody has read what the next loads replace
+        auto landed = [&](int kt, int behind) __attribute__((always_inline)) {
+            static_assert(T::NS <= 4, "waits");
+            if (T::NS >= 4 && behind >= 3)
+                wait_vmcnt<3 * LPS>();
+            else if (T::NS >= 4 && behind == 2)
+                wait_vmcnt<2 * LPS>();
+            else if (T::NS >= 3 && behind == 2)
+                wait_vmcnt<2 * LPS>();
+            else if (behind == 1)
+                wait_vmcnt<LPS>();
+            else
+                wait_vmcnt<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
+            if (OP == kFfnDw && kt == nk - 1 && used % STEPS) {
+                // the steps past the expert's last row: zeros in both operands, whatever lies there
+                char *stage = stages + kt % T::NS * T::STAGE;
+                const int from = used % STEPS;
+                for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += T::THREADS) *(u32x4_t *)(stage + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+                for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += T::THREADS)
+                    *(u32x4_t *)(stage + OA::BYTES + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+                __syncthreads();
+            }
+        };
+        landed(0, min(nk, T::NS) - 1);
+        char *stage = stages;
+        auto first_steps = [&](auto loads) __attribute__((always_inline)) {  // of a stage: all but the last
+#pragma unroll
+            for (int kk = 0; kk + 1 < KK; ++kk) {
+                if (kk & 1)
+                    step(stage, kk + 1, f0, f1, loads, kk + 1);
+                else
+                    step(stage, kk + 1, f1, f0, loads, kk + 1);
+            }
+        };
+        auto on = [&]() __attribute__((always_inline)) {
+            stage += T::STAGE;
+            if (stage == stages + T::NS * T::STAGE) stage = stages;
+        };
+        read(stage, 0, f0);
+        first_steps(std::false_type{});
+        int kt = 1;
+        for (; kt <= nk - T::NS; ++kt) {  // (T::NS - 2 stages are in flight behind this one)
+            landed(kt, T::NS - 2);
+            on();
+            begin_stage();
+            step(stage, 0, f0, f1, std::true_type{}, 0);
+            first_steps(std::true_type{});
+            end_stage();
         }
+        for (; kt < nk; ++kt) {
+            landed(kt, min(nk - 1 - kt, T::NS - 2));
+            on();
+            step(stage, 0, f0, f1, std::false_type{}, 0);
+            first_steps(std::false_type{});
+        }
+        ask();  // (no load is in flight any more: the wait for the answer holds nothing up)
+#pragma unroll
+        for (int mb = 0; mb < LIVE; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(f1.b[nb], f1.a[mb], acc[mb][nb]);
+        answer();
+        __syncthreads();
     };
 
-    // ---- out.  128 bytes of 32 rows (64 columns of bf16, 32 of fp32; less where a wavefront has less) go through LDS of the wavefront's own: the
-    // matrix cores leave lane l with row l & 31, columns 8 q + 4 (l >> 5) + 0..3 of a block; memory is reached in pieces of 16 bytes.
+    // ---- out.  The matrix cores leave lane l of a block with row l & 31 and columns 8 q + 4 (l >> 5) + 0..3, q = 0..3: 16 bytes of fp32, but 8 of
+    // bf16, where the halves of a wavefront swap what they have of two q, so that lanes below 32 have 16 bytes of one and the others of the other.
     constexpr int COL_BLOCKS = GATED ? T::NB / 2 : T::NB;
-    constexpr int GROUP = SZ == 2 && COL_BLOCKS % 2 == 0 ? 2 : 1;  // blocks at a time
-    constexpr int LANES = GROUP * 32 / PIECE, ROWS = 64 / LANES;  // lanes per row, rows at a time
-    char *out = smem + T::AT_OUT + wave * T::OUT;
-    typedef u32x4_t __attribute__((may_alias)) Piece16;
-    typedef __attribute__((ext_vector_type(2))) u32 u32x2_t;
-    typedef u32x2_t __attribute__((may_alias)) Piece8;
+    constexpr int PIECES = 32 * SZ / 32;  // pieces of 16 bytes that a lane has of a block: 2 of bf16, 4 of fp32
+    auto pieces_of = [&](auto value, u32x4_t (&v)[PIECES]) __attribute__((always_inline)) {  // value(register)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            if constexpr (SZ == 2) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(value(8 * i + 2 * j), value(8 * i + 2 * j + 1)),
+                                                                    pack_bf16x2(value(8 * i + 4 + 2 * j), value(8 * i + 4 + 2 * j + 1)), false, false);
+                    v[i][j] = x[0], v[i][2 + j] = x[1];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = __float_as_uint(value(4 * i + j));
+            }
+        }
+    };
+    auto values_of = [&](const u32x4_t (&v)[PIECES], float (&x)[16]) __attribute__((always_inline)) {  // the other way
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            if constexpr (SZ == 2) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const auto y = __builtin_amdgcn_permlane32_swap(v[i][j], v[i][2 + j], false, false);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) x[8 * i + 4 * h + 2 * j] = __uint_as_float(y[h] << 16), x[8 * i + 4 * h + 2 * j + 1] = __uint_as_float(y[h] & 0xffff0000u);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[4 * i + j] = __uint_as_float(v[i][j]);
+            }
+        }
+    };
     auto write_tile = [&](const Tile &w) __attribute__((always_inline)) {
         const int rows = DW ? a.M : w.s.extent;
 #pragma unroll
         for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
-            for (int gb = 0; gb < COL_BLOCKS; gb += GROUP) {
-                __builtin_amdgcn_sched_barrier(0);  // (results of one group at a time: registers)
-                const int m0 = w.row0 + (wm * T::MB + mb) * 32, n0 = w.n0 + (wn * COL_BLOCKS + gb) * 32;
+            for (int nb = 0; nb < COL_BLOCKS; ++nb) {
+                __builtin_amdgcn_sched_barrier(0);  // (results of one block at a time: registers)
+                const int m0 = w.row0 + (wm * T::MB + mb) * 32, n0 = w.n0 + (wn * COL_BLOCKS + nb) * 32;
                 if (n0 >= a.N || m0 >= rows) continue;
-                const size_t first = DW ? 0 : (size_t)w.s.begin;
-                // (or the places and sums of all groups are fetched ahead into vector registers, and spilled)
+                // (or the places and sums of all blocks are fetched ahead into vector registers, and spilled)
                 int l = lane;
                 asm volatile("" : "+v"(l));
+                asm volatile("" : "+a"(acc[mb][nb]));
+                if (GATED) asm volatile("" : "+a"(acc[mb][nb + T::NB / 2]));
+                const int m = m0 + (l & 31), n = n0 + (l >> 5) * PIECE;  // and 2 * PIECE columns further from piece to piece
+                const bool in = m < rows, used = DW || m < w.s.used;
+                const size_t row = (DW ? 0 : (size_t)w.s.begin) + m;
+                auto put = [&](auto value, void *to, long long ld) __attribute__((always_inline)) {
+                    u32x4_t v[PIECES];
+                    pieces_of(value, v);
+                    u32x4_t *p = (u32x4_t *)((ET *)to + row * ld + n);
 #pragma unroll
-                for (int b = 0; b < GROUP; ++b) {
-                    asm volatile("" : "+a"(acc[mb][gb + b]));
-                    if (GATED) asm volatile("" : "+a"(acc[mb][gb + b + T::NB / 2]));
-                }
-                const int out_r = l / LANES, out_c = l % LANES * PIECE;
-                // f(row of the matrix, column, number of the piece) where there are such elements
-                auto each_piece = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int i = 0; i < 32 / ROWS; ++i) {
-                        const int m = m0 + i * ROWS + out_r, n = n0 + out_c;
-                        if (n < a.N && m < rows) f(m, first + m, n, i);
+                    for (int i = 0; i < PIECES; ++i) {
+                        if (!used) v[i] = u32x4_t{0, 0, 0, 0};  // (an unused row has the sums of a used one)
+                        if (in && n + 2 * PIECE * i < a.N) p[2 * i] = v[i];
                     }
                 };
-                auto put = [&](auto value, void *to, long long ld) __attribute__((always_inline)) {  // value(block, register)
-                    asm volatile("" ::: "memory");
-#pragma unroll
-                    for (int b = 0; b < GROUP; ++b)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            char *p = out + (l & 31) * T::OUT_ROW + (b * 32 + q * 8 + (l >> 5) * 4) * SZ;
-                            const float v[4] = {value(b, 4 * q), value(b, 4 * q + 1), value(b, 4 * q + 2), value(b, 4 * q + 3)};
-                            if constexpr (SZ == 2)
-                                *(Piece8 *)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                            else
-                                *(Piece16 *)p = Piece<float>::pack(v);
-                        }
-                    asm volatile("" ::: "memory");
-                    each_piece([&](int m, size_t row, int n, int i) __attribute__((always_inline)) {
-                        u32x4_t v = *(const Piece16 *)(out + (i * ROWS + out_r) * T::OUT_ROW + out_c * SZ);
-                        if (!DW && m >= w.s.used) v = u32x4_t{0, 0, 0, 0};  // (an unused row has the sums of a used one)
-                        *(Piece16 *)((ET *)to + row * ld + n) = v;
-                    });
-                };
+                auto sum = [&](int i) __attribute__((always_inline)) { return acc[mb][nb][i]; };
                 if constexpr (OP == kFfnUp) {
-                    auto g = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; };
-                    auto u = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b + T::NB / 2][i]; };
-                    if (a.o0) put(g, a.o0, a.ldo), put(u, a.o1, a.ldo);
-                    if (a.o2) put([&](int b, int i) __attribute__((always_inline)) { return g(b, i) * sigmoid<ET>(g(b, i)) * u(b, i); }, a.o2, a.N);
+                    auto u = [&](int i) __attribute__((always_inline)) { return acc[mb][nb + T::NB / 2][i]; };
+                    if (a.o0) put(sum, a.o0, a.ldo), put(u, a.o1, a.ldo);
+                    if (a.o2) put([&](int i) __attribute__((always_inline)) { return sum(i) * sigmoid<ET>(sum(i)) * u(i); }, a.o2, a.N);
                 } else if constexpr (OP == kFfnDh) {
-                    auto dh = [&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; };
-                    if (a.o2) put(dh, a.o2, a.N);
+                    if (a.o2) put(sum, a.o2, a.N);
                     if (!a.o0) continue;
-                    u32x4_t gv[32 / ROWS] = {}, uv[32 / ROWS] = {};
-                    each_piece([&](int, size_t row, int n, int i) __attribute__((always_inline)) {
-                        gv[i] = *(const Piece16 *)((const ET *)a.g + row * a.ldg + n), uv[i] = *(const Piece16 *)((const ET *)a.u + row * a.ldg + n);
-                    });
-                    float s[GROUP * 16], u[GROUP * 16];
-                    auto take = [&](const u32x4_t (&v)[32 / ROWS], float *x) __attribute__((always_inline)) {  // pieces to where the sums are
-                        asm volatile("" ::: "memory");
+                    u32x4_t v[PIECES], w[PIECES];
+                    const size_t at = row * a.ldg + n;
 #pragma unroll
-                        for (int i = 0; i < 32 / ROWS; ++i) *(Piece16 *)(out + (i * ROWS + out_r) * T::OUT_ROW + out_c * SZ) = v[i];
-                        asm volatile("" ::: "memory");
-#pragma unroll
-                        for (int b = 0; b < GROUP; ++b)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const char *p = out + (l & 31) * T::OUT_ROW + (b * 32 + q * 8 + (l >> 5) * 4) * SZ;
-                                if constexpr (SZ == 2) {
-                                    const u32x2_t y = *(const Piece8 *)p;
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j) x[b * 16 + 4 * q + j] = __uint_as_float(j & 1 ? y[j / 2] & 0xffff0000u : y[j / 2] << 16);
-                                } else {
-                                    Piece<float>::unpack(*(const Piece16 *)p, x + b * 16 + 4 * q);
-                                }
-                            }
-                    };
-                    take(gv, s);
-                    take(uv, u);
-#pragma unroll
-                    for (int i = 0; i < GROUP * 16; ++i) {
-                        const float g = s[i], sg = sigmoid<ET>(g);
-                        s[i] = g * sg;
-                        u[i] = u[i] * (sg * (1.f + g * (1.f - sg)));
+                    for (int i = 0; i < PIECES; ++i) {
+                        v[i] = w[i] = u32x4_t{0, 0, 0, 0};
+                        if (in && n + 2 * PIECE * i < a.N)
+                            v[i] = *(const u32x4_t *)((const ET *)a.g + at + 2 * PIECE * i), w[i] = *(const u32x4_t *)((const ET *)a.u + at + 2 * PIECE * i);
                     }
-                    put([&](int b, int i) __attribute__((always_inline)) { return dh(b, i) * u[b * 16 + i]; }, a.o0, a.ldo);
-                    put([&](int b, int i) __attribute__((always_inline)) { return dh(b, i) * s[b * 16 + i]; }, a.o1, a.ldo);
+                    float g[16], u[16];
+                    values_of(v, g);
+                    values_of(w, u);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float s = sigmoid<ET>(g[i]);
+                        u[i] = u[i] * (s * (1.f + g[i] * (1.f - s)));
+                        g[i] = g[i] * s;
+                    }
+                    put([&](int i) __attribute__((always_inline)) { return sum(i) * u[i]; }, a.o0, a.ldo);
+                    put([&](int i) __attribute__((always_inline)) { return sum(i) * g[i]; }, a.o1, a.ldo);
                 } else if constexpr (DW) {
-                    put([&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; }, (ET *)(w.matrix ? a.o1 : a.o0) + (size_t)w.s.e * a.eo, a.ldo);
+                    put(sum, (ET *)(w.matrix ? a.o1 : a.o0) + (size_t)w.s.e * a.eo, a.ldo);
                 } else {
-                    put([&](int b, int i) __attribute__((always_inline)) { return acc[mb][gb + b][i]; }, a.o0, a.N);
+                    put(sum, a.o0, a.N);
                 }
             }
         __builtin_amdgcn_sched_barrier(0);
     };
 
     // The next tile's first stages are on their way while this one's results go out.
-    Tile now = tile_at(range.next);
+    Tile now = tile_at(tile);
     start(now);
     while (true) {
 #pragma unroll
@@ -525,50 +616,33 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[mb][nb][v] = 0.f;
         if (nk) {
-            landed(0, min(nk, T::NS) - 1);
-            char *stage = stages;
-            auto first_steps = [&](auto loads) __attribute__((always_inline)) {  // of a stage: all but the last
-#pragma unroll
-                for (int kk = 0; kk + 1 < KK; ++kk) {
-                    if (kk & 1)
-                        step(stage, kk + 1, f0, f1, loads, kk + 1);
-                    else
-                        step(stage, kk + 1, f1, f0, loads, kk + 1);
-                }
-            };
-            auto on = [&]() __attribute__((always_inline)) {
-                stage += T::STAGE;
-                if (stage == stages + T::NS * T::STAGE) stage = stages;
-            };
-            read(stage, 0, f0);
-            first_steps(std::false_type{});
-            int kt = 1;
-            for (; kt <= nk - T::NS; ++kt) {  // (T::NS - 2 stages are in flight behind this one)
-                landed(kt, T::NS - 2);
-                on();
-                begin_stage();
-                step(stage, 0, f0, f1, std::true_type{}, 0);
-                first_steps(std::true_type{});
-                end_stage();
+            if constexpr (SHORT) {
+                if (live == T::MB)
+                    products(std::integral_constant<int, T::MB>{});
+                else if (live == T::MB / 4 * 3)
+                    products(std::integral_constant<int, T::MB / 4 * 3>{});
+                else if (live == T::MB / 2)
+                    products(std::integral_constant<int, T::MB / 2>{});
+                else
+                    products(std::integral_constant<int, T::MB / 4>{});
+            } else {
+                products(std::integral_constant<int, T::MB>{});
             }
-            for (; kt < nk; ++kt) {
-                landed(kt, min(nk - 1 - kt, T::NS - 2));
-                on();
-                step(stage, 0, f0, f1, std::false_type{}, 0);
-                first_steps(std::false_type{});
-            }
-#pragma unroll
-            for (int mb = 0; mb < T::MB; ++mb)
-#pragma unroll
-                for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(f1.b[nb], f1.a[mb], acc[mb][nb]);
+        }
+        else {
+            ask();
+            __syncthreads();  // (everybody has read the answer before)
+            answer();
             __syncthreads();
         }
-        range.next += range.step;
-        const bool more = range.next < range.to;
+        if (a.plan)
+            tile = uniform(tables->next);
+        else if ((tile += per_list) >= uniform(tables->edge[list + 1]))
+            tile = -1;
         const Tile done = now;
-        if (more) now = tile_at(range.next), start(now);
+        if (tile >= 0) now = tile_at(tile), start(now);
         write_tile(done);
-        if (!more) break;
+        if (tile < 0) break;
     }
 }
 

@@ -26,8 +26,18 @@ static int compute_units(int *n) {
     return MOE_OK;
 }
 
+// How a product is launched: workgroups, and whether their tiles are planned.
+struct Launch {
+    const void *kernel;
+    unsigned groups, smem;
+    int bm;
+    bool planned;
+};
+// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own.
+constexpr int kPlannedTiles = 2;
+
 template <class T, FfnOp OP>
-static int launch(FfnArgs a, hipStream_t st) {
+static int prepare(FfnArgs &a, Launch *l) {
     constexpr int COLS = OP == kFfnUp ? T::BN / 2 : T::BN;
     a.nt = (a.N + COLS - 1) / COLS * (OP == kFfnDw && a.o1 ? 2 : 1);
     a.mt = (a.M + T::BM - 1) / T::BM;
@@ -44,17 +54,21 @@ static int launch(FfnArgs a, hipStream_t st) {
     if (const int rc = compute_units(&cus)) return rc;
     if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
     const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * (160 * 1024 / T::SMEM);
-    hipLaunchKernelGGL((k_ffn<T, OP>), dim3((unsigned)(tiles < room ? tiles : room)), dim3(T::THREADS), T::SMEM, st, a);
-    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+    l->kernel = (const void *)k_ffn<T, OP>;
+    l->groups = (unsigned)(tiles < room ? tiles : room);
+    l->smem = T::SMEM;
+    l->bm = T::BM;
+    l->planned = tiles >= kPlannedTiles * room;
+    return MOE_OK;
 }
 
 template <typename ET, FfnOp OP>
-static int pick(const FfnArgs &a, int slots, hipStream_t st) {
+static int pick(FfnArgs &a, int slots, Launch *l) {
     if constexpr (sizeof(ET) == 4) {
-        return slots / a.E > 48 ? launch<FfnTile<ET, 2, 2, 2, 2, 64, 4>, OP>(a, st) : launch<FfnTile<ET, 1, 2, 1, 4, 64, 4>, OP>(a, st);
+        return slots / a.E > 48 ? prepare<FfnTile<ET, 2, 2, 2, 2, 64, 4>, OP>(a, l) : prepare<FfnTile<ET, 1, 2, 1, 4, 64, 4>, OP>(a, l);
     } else {
 #ifndef V256
-#define V256 4, 4, 2, 2, 64, 4
+#define V256 8, 2, 1, 4, 64, 4
 #endif
 #ifndef V128
 #define V128 2, 4, 2, 2, 64, 4
@@ -62,24 +76,51 @@ static int pick(const FfnArgs &a, int slots, hipStream_t st) {
 #ifndef V32
 #define V32 1, 2, 1, 4, 128, 3
 #endif
-        if (slots / a.E > 160) return launch<FfnTile<ET, V256>, OP>(a, st);
-        return slots / a.E > 48 ? launch<FfnTile<ET, V128>, OP>(a, st) : launch<FfnTile<ET, V32>, OP>(a, st);
+        if (slots / a.E > 160) return prepare<FfnTile<ET, V256>, OP>(a, l);
+        return slots / a.E > 48 ? prepare<FfnTile<ET, V128>, OP>(a, l) : prepare<FfnTile<ET, V32>, OP>(a, l);
     }
 }
 template <typename ET>
-static int pick_dw(const FfnArgs &a, hipStream_t st) {
+static int pick_dw(FfnArgs &a, Launch *l) {
     if constexpr (sizeof(ET) == 4)
-        return launch<FfnTile<ET, 2, 2, 2, 2, 64, 4>, kFfnDw>(a, st);
+        return prepare<FfnTile<ET, 2, 2, 2, 2, 64, 4>, kFfnDw>(a, l);
     else
-        return launch<FfnTile<ET, V256>, kFfnDw>(a, st);
+#ifndef VDW
+#define VDW 4, 4, 2, 2, 64, 4
+#endif
+        return prepare<FfnTile<ET, VDW>, kFfnDw>(a, l);
 }
 template <FfnOp OP>
-static int pick(const moe_problem_t *p, const FfnArgs &a, void *stream) {
-    hipStream_t st = (hipStream_t)stream;
+static int pick(const moe_problem_t *p, FfnArgs &a, Launch *l) {
     if constexpr (OP == kFfnDw)
-        return p->dtype == MOE_DT_F32 ? pick_dw<float>(a, st) : pick_dw<bf16_t>(a, st);
+        return p->dtype == MOE_DT_F32 ? pick_dw<float>(a, l) : pick_dw<bf16_t>(a, l);
     else
-        return p->dtype == MOE_DT_F32 ? pick<float, OP>(a, p->T * p->k, st) : pick<bf16_t, OP>(a, p->T * p->k, st);
+        return p->dtype == MOE_DT_F32 ? pick<float, OP>(a, p->T * p->k, l) : pick<bf16_t, OP>(a, p->T * p->k, l);
+}
+// A call's launches: a product of rows (any but dw), dw, or both.
+template <FfnOp OP>
+static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *workspace, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    Launch l[2] = {};
+    FfnArgs *a[2] = {rows, dw};
+    if (rows)
+        if (const int rc = pick<OP>(p, *rows, &l[0])) return rc;
+    if (dw)
+        if (const int rc = pick<kFfnDw>(p, *dw, &l[1])) return rc;
+    FfnPlan *plans = (FfnPlan *)workspace;
+    if (l[0].planned || l[1].planned) {
+        FfnPlanArgs plan = {};
+        if (l[0].planned) plan.rows = *rows, plan.rows_plan = plans, plan.bm = l[0].bm, rows->plan = plans;
+        if (l[1].planned) plan.dw = *dw, plan.dw_plan = plans + 1, dw->plan = plans + 1;
+        hipLaunchKernelGGL(k_ffn_plan, dim3(1), dim3(kThreads), 0, st, plan);
+        if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (!a[i]) continue;
+        void *args[] = {a[i]};
+        if (hipLaunchKernel(l[i].kernel, dim3(l[i].groups), dim3(kThreads), args, l[i].smem, st) != hipSuccess) return MOE_ERR_HIP;
+    }
+    return MOE_OK;
 }
 static FfnArgs args_of(const moe_problem_t *p, const int32_t *counts) {
     FfnArgs a = {};
@@ -89,7 +130,7 @@ static FfnArgs args_of(const moe_problem_t *p, const int32_t *counts) {
 
 extern "C" {
 
-size_t moe_ffn_workspace_bytes(const moe_problem_t *p) { return check_problem(p) == MOE_OK ? 256 : 0; }
+size_t moe_ffn_workspace_bytes(const moe_problem_t *p) { return check_problem(p) == MOE_OK ? (2 * sizeof(FfnPlan) + 255) / 256 * 256 : 0; }
 
 static int check_workspace(const void *ws) { return !ws || ((uintptr_t)ws & 255) != 0 ? MOE_ERR_WORKSPACE : MOE_OK; }
 
@@ -106,7 +147,7 @@ int moe_ffn_up(const moe_problem_t *p, const void *x_perm, const void *W1, const
     a.A0 = x_perm; a.lda = p->d;
     a.B0 = W1; a.B1 = W3; a.ldb = ldw; a.eb = (long long)p->d * ldw;
     a.o0 = g; a.o1 = u; a.ldo = ld; a.o2 = h;
-    return pick<kFfnUp>(p, a, stream);
+    return launch<kFfnUp>(p, &a, nullptr, workspace, stream);
 }
 
 int moe_ffn_down(const moe_problem_t *p, const void *h, const void *W2, const int32_t *counts, void *y, void *workspace, void *stream) {
@@ -120,7 +161,7 @@ int moe_ffn_down(const moe_problem_t *p, const void *h, const void *W2, const in
     a.A0 = h; a.lda = p->f;
     a.B0 = W2; a.ldb = p->d; a.eb = (long long)p->f * p->d;
     a.o0 = y;
-    return pick<kFfnDown>(p, a, stream);
+    return launch<kFfnDown>(p, &a, nullptr, workspace, stream);
 }
 
 int moe_ffn_down_backward(const moe_problem_t *p, const void *dy, const void *W2, const void *h, const void *g, const void *u, const int32_t *counts,
@@ -134,22 +175,23 @@ int moe_ffn_down_backward(const moe_problem_t *p, const void *dy, const void *W2
         !aligned16(dW2))
         return MOE_ERR_INVALID_ARG;
     if ((rc = check_workspace(workspace))) return rc;
-    if (dh || dg) {
-        FfnArgs a = args_of(p, counts);
+    FfnArgs rows = args_of(p, counts), dw = rows;
+    {
+        FfnArgs &a = rows;
         a.N = p->f; a.K = p->d;
         a.A0 = dy; a.lda = p->d;
         a.B0 = W2; a.ldb = p->d; a.eb = (long long)p->f * p->d;
         a.g = g; a.u = u; a.ldg = ld;
         a.o0 = dg; a.o1 = du; a.ldo = ld; a.o2 = dh;
-        if ((rc = pick<kFfnDh>(p, a, stream))) return rc;
     }
-    if (!dW2) return MOE_OK;
-    FfnArgs a = args_of(p, counts);
-    a.M = p->f; a.N = p->d;
-    a.A0 = h; a.lda = p->f;
-    a.B0 = dy; a.ldb = p->d;
-    a.o0 = dW2; a.ldo = p->d; a.eo = (long long)p->f * p->d;
-    return pick<kFfnDw>(p, a, stream);
+    {
+        FfnArgs &a = dw;
+        a.M = p->f; a.N = p->d;
+        a.A0 = h; a.lda = p->f;
+        a.B0 = dy; a.ldb = p->d;
+        a.o0 = dW2; a.ldo = p->d; a.eo = (long long)p->f * p->d;
+    }
+    return launch<kFfnDh>(p, dh || dg ? &rows : nullptr, dW2 ? &dw : nullptr, workspace, stream);
 }
 
 int moe_ffn_up_backward(const moe_problem_t *p, const void *x_perm, const void *W1, const void *W3, int64_t ldw, const void *dg, const void *du,
@@ -162,21 +204,22 @@ int moe_ffn_up_backward(const moe_problem_t *p, const void *x_perm, const void *
     if (!aligned16(x_perm) || !aligned16(W1) || !aligned16(W3) || !aligned16(dg) || !aligned16(du) || !aligned16(dx) || !aligned16(dW1) || !aligned16(dW3))
         return MOE_ERR_INVALID_ARG;
     if ((rc = check_workspace(workspace))) return rc;
-    if (dx) {
-        FfnArgs a = args_of(p, counts);
+    FfnArgs rows = args_of(p, counts), dw = rows;
+    {
+        FfnArgs &a = rows;
         a.N = p->d; a.K = p->f;
         a.A0 = dg; a.A1 = du; a.lda = ld;
         a.B0 = W1; a.B1 = W3; a.ldb = ldw; a.eb = (long long)p->d * ldw;
         a.o0 = dx;
-        if ((rc = pick<kFfnDx>(p, a, stream))) return rc;
     }
-    if (!dW1 && !dW3) return MOE_OK;
-    FfnArgs a = args_of(p, counts);
-    a.M = p->d; a.N = p->f;
-    a.A0 = x_perm; a.lda = p->d;
-    a.B0 = dW1 ? dg : du; a.B1 = du; a.ldb = ld;
-    a.o0 = dW1 ? dW1 : dW3; a.o1 = dW1 ? dW3 : nullptr; a.ldo = ldw; a.eo = (long long)p->d * ldw;
-    return pick<kFfnDw>(p, a, stream);
+    {
+        FfnArgs &a = dw;
+        a.M = p->d; a.N = p->f;
+        a.A0 = x_perm; a.lda = p->d;
+        a.B0 = dW1 ? dg : du; a.B1 = du; a.ldb = ld;
+        a.o0 = dW1 ? dW1 : dW3; a.o1 = dW1 ? dW3 : nullptr; a.ldo = ldw; a.eo = (long long)p->d * ldw;
+    }
+    return launch<kFfnDx>(p, dx ? &rows : nullptr, dW1 || dW3 ? &dw : nullptr, workspace, stream);
 }
 
 }  // extern "C"
