@@ -84,15 +84,17 @@ struct FfnPlan {
     mutable Counter taken[kTileQueues];  // tiles handed out of an XCD's list, beyond the first ones
 };
 
-// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts, stages of KB bytes of the reduction, NS of them.
-template <typename ET_, int MB_, int NB_, int WM_, int WN_, int KB_, int NS_>
+// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts (row blocks go round those of a column), stages of KB bytes of the reduction, as
+// many as fit the LDS of OCC workgroups per CU.
+template <typename ET_, int MB_, int NB_, int WM_, int WN_, int KB_, int OCC_>
 struct FfnTile {
     typedef ET_ ET;
-    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KB = KB_, NS = NS_, WAVES = WM * WN, THREADS = 64 * WAVES;
-    static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * KB;
-    static constexpr int AT_TABLES = NS * STAGE;
-    static constexpr int SMEM = AT_TABLES + (int)sizeof(FfnTables);
-    static_assert(SMEM <= 160 * 1024, "LDS");
+    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KB = KB_, OCC = OCC_, WAVES = WM * WN;
+    static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN;
+    static constexpr int ROOM = (160 * 1024 / OCC - (int)sizeof(FfnTables)) / 1024 * 1024, SMEM = ROOM + (int)sizeof(FfnTables);
+    static constexpr int stage_bytes(int live) { return (BN + BM / MB * live) * KB; }  // of a tile with `live` row blocks per wavefront
+    static constexpr int stages(int live) { return ROOM / stage_bytes(live) < 7 ? ROOM / stage_bytes(live) : 7; }
+    static_assert(WAVES * 64 == kThreads, "threads");
 };
 
 __device__ __forceinline__ u64 scan_workgroup(u64 v, u64 *lds, u64 *total) {  // inclusive, kThreads threads
@@ -212,6 +214,20 @@ __device__ __forceinline__ void read_frags(const char *stage, int kk, const int 
         }
     }
 }
+// Until no more than the loads of `behind` stages, LPS each, are in flight.
+template <int MOST, int LPS>
+__device__ __forceinline__ void wait_behind(int behind) {
+    if constexpr (MOST <= 0) {
+        wait_vmcnt<0>();
+    } else {
+        static_assert(MOST * LPS <= 63, "vmcnt range");
+        if (behind >= MOST)
+            wait_vmcnt<MOST * LPS>();
+        else
+            wait_behind<MOST - 1, LPS>(behind);
+    }
+}
+
 template <typename ET>
 __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32x16_t &acc) {
     if constexpr (sizeof(ET) == 2) {
@@ -223,7 +239,7 @@ __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32
 }
 
 template <class T, FfnOp OP>
-__global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
+__global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     typedef typename T::ET ET;
     constexpr bool DW = OP == kFfnDw, AK = !DW, BK = OP == kFfnDh || OP == kFfnDx, GATED = OP == kFfnUp;
     typedef Operand<ET, T::BM, AK, T::KB, T::WAVES> OA;
@@ -233,9 +249,8 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     static_assert(!GATED || T::NB % 2 == 0, "g and u of the same columns");
     extern __shared__ __align__(128) char smem[];
     char *stages = smem;
-    FfnTables *tables = (FfnTables *)(smem + T::AT_TABLES);
+    FfnTables *tables = (FfnTables *)(smem + T::ROOM);
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
-    static_assert(T::THREADS == kThreads, "four wavefronts");
     if (a.plan) {
         for (int i = tid; i < (int)(sizeof(FfnTables) / 4); i += kThreads) ((u32 *)tables)[i] = ((const u32 *)&a.plan->tables)[i];
         __syncthreads();
@@ -301,8 +316,8 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
         return w;
     };
 
-    // Row blocks that are not full: loops of their own for a quarter, a half and three quarters of the rows.  (A wavefront has all rows then.)
-    constexpr bool SHORT = !DW && T::WM == 1 && T::MB % 4 == 0;
+    // Row blocks that are not full have loops of their own, for a quarter, a half and three quarters of the rows, and more stages in flight.
+    constexpr bool SHORT = !DW && T::MB % 4 == 0;
     auto loads_of_a = [](int live) __attribute__((always_inline)) { return (OA::INSTR * live / T::MB + T::WAVES - 1) / T::WAVES; };
 
     // ---- loads.  A lane's places in the operands; they go on from stage to stage.
@@ -311,7 +326,8 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     const size_t a_step = AK ? T::KB : STEPS * lda, b_step = BK ? T::KB : STEPS * ldb;
     const u32 lds = lds_offset(stages);
     int next, nk, used;  // the stage to load; stages and rows of the tile that is loaded
-    int live, a_loads;   // blocks of 32 rows it has (LIVES), loads of A per wavefront
+    int live, a_loads;   // row blocks per wavefront it has, loads of A per wavefront
+    u32 stage_bytes, to_end;
     u32 to;              // where it goes
     // before a stage's loads: on to the second pair of operands; rows past the expert's last one are that one again
     auto begin_stage = [&]() __attribute__((always_inline)) {
@@ -332,18 +348,18 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     };
     auto load_one = [&](int i) __attribute__((always_inline)) {
         if (i < OA::PER_WAVE) {
-            load_to_lds(ap[i], to + OA::instr(wave, i) * 1024);
+            load_to_lds(ap[i], to + OB::BYTES + OA::instr(wave, i) * 1024);
             ap[i] += a_step;
         } else {
             const int j = i - OA::PER_WAVE;
-            load_to_lds(bp[j], to + OA::BYTES + OB::instr(wave, j) * 1024);
+            load_to_lds(bp[j], to + OB::instr(wave, j) * 1024);
             bp[j] += b_step;
         }
     };
     auto end_stage = [&]() __attribute__((always_inline)) {
         ++next;
-        to += T::STAGE;
-        if (to == lds + T::NS * T::STAGE) to = lds;
+        to += stage_bytes;
+        if (to == to_end) to = lds;
     };
     auto load_stage = [&]() __attribute__((always_inline)) {
         begin_stage();
@@ -361,7 +377,9 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
         if (!nk) return;
         const int rows = used - w.row0;
         live = !SHORT || rows > T::BM / 4 * 3 ? T::MB : rows > T::BM / 2 ? T::MB / 4 * 3 : rows > T::BM / 4 ? T::MB / 2 : T::MB / 4;
-        a_loads = loads_of_a(live);
+        a_loads = loads_of_a(live), stage_bytes = T::stage_bytes(live);
+        const int ns = live == T::MB ? T::stages(T::MB) : live == T::MB / 4 * 3 ? T::stages(T::MB / 4 * 3) : live == T::MB / 2 ? T::stages(T::MB / 2) : T::stages(T::MB / 4);
+        to_end = lds + ns * stage_bytes;
         const char *A = (const char *)a.A0, *B = (const char *)(DW && w.matrix ? a.B1 : a.B0);
 #pragma unroll
         for (int i = 0; i < OA::PER_WAVE; ++i) {
@@ -387,7 +405,7 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
                 bp[i] = from + first + (size_t)r * ldb + (size_t)(n < a.N ? n : 0) * SZ;
             }
         }
-        const int ahead = min(nk, T::NS);
+        const int ahead = min(nk, ns);
         for (int i = 0; i < ahead; ++i) load_stage();
     };
 
@@ -395,7 +413,7 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     f32x16_t acc[T::MB][T::NB];
     int a_at[T::MB], b_at[T::NB];
 #pragma unroll
-    for (int mb = 0; mb < T::MB; ++mb) a_at[mb] = (wm * T::MB + mb) * 32;
+    for (int mb = 0; mb < T::MB; ++mb) a_at[mb] = (mb * T::WM + wm) * 32;
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb)
         b_at[nb] = !GATED ? (wn * T::NB + nb) * 32 : nb < T::NB / 2 ? (wn * T::NB / 2 + nb) * 32 : COLS + (wn * T::NB / 2 + nb - T::NB / 2) * 32;
@@ -405,7 +423,8 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     constexpr int KK = T::KB / 32;  // steps per stage
     static_assert(KK % 2 == 0, "two sets of fragments in turn");
     auto products = [&](auto blocks) __attribute__((always_inline)) {
-        constexpr int LIVE = decltype(blocks)::value;
+        constexpr int LIVE = decltype(blocks)::value, NS = T::stages(LIVE), STAGE = T::stage_bytes(LIVE);
+        static_assert(NS >= 2, "stages");
         constexpr int AL = (OA::INSTR * LIVE / T::MB + T::WAVES - 1) / T::WAVES, LPS = AL + OB::PER_WAVE;  // loads per wavefront and stage
         constexpr int LPK = (LPS + KK - 1) / KK;
         constexpr int NREAD = LIVE * OA::READS + T::NB * OB::READS, NMUL = LIVE * T::NB, NMFMA = NMUL * (SZ == 2 ? 1 : 4);
@@ -414,8 +433,8 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
         };
         Frags f0, f1;
         auto read = [&](const char *stage, int kk, Frags &f) __attribute__((always_inline)) {
-            read_frags<OA>(stage, kk, a_at, lane, f.a);
-            read_frags<OB>(stage + OA::BYTES, kk, b_at, lane, f.b);
+            read_frags<OA>(stage + OB::BYTES, kk, a_at, lane, f.a);
+            read_frags<OB>(stage, kk, b_at, lane, f.b);
         };
         // products of `cur`, with the reads of `nxt` and, if LOADS, share `part` of a stage's loads in between
         auto step = [&](const char *stage, int kk, Frags &nxt, const Frags &cur, auto loads, int part) __attribute__((always_inline)) {
@@ -442,30 +461,20 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
         };
         // stage kt has landed, and everybody has read what the next loads replace
         auto landed = [&](int kt, int behind) __attribute__((always_inline)) {
-            static_assert(T::NS <= 4, "waits");
-            if (T::NS >= 4 && behind >= 3)
-                wait_vmcnt<3 * LPS>();
-            else if (T::NS >= 4 && behind == 2)
-                wait_vmcnt<2 * LPS>();
-            else if (T::NS >= 3 && behind == 2)
-                wait_vmcnt<2 * LPS>();
-            else if (behind == 1)
-                wait_vmcnt<LPS>();
-            else
-                wait_vmcnt<0>();
+            wait_behind<NS - 1, LPS>(behind);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
             if (OP == kFfnDw && kt == nk - 1 && used % STEPS) {
                 // the steps past the expert's last row: zeros in both operands, whatever lies there
-                char *stage = stages + kt % T::NS * T::STAGE;
+                char *stage = stages + kt % NS * STAGE;
                 const int from = used % STEPS;
-                for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += T::THREADS) *(u32x4_t *)(stage + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
-                for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += T::THREADS)
-                    *(u32x4_t *)(stage + OA::BYTES + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+                for (int i = tid; i < (STEPS - from) * (T::BM * SZ / 16); i += kThreads) *(u32x4_t *)(stage + OB::BYTES + from * T::BM * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
+                for (int i = tid; i < (STEPS - from) * (T::BN * SZ / 16); i += kThreads)
+                    *(u32x4_t *)(stage + from * T::BN * SZ + i * 16) = u32x4_t{0, 0, 0, 0};
                 __syncthreads();
             }
         };
-        landed(0, min(nk, T::NS) - 1);
+        landed(0, min(nk, NS) - 1);
         char *stage = stages;
         auto first_steps = [&](auto loads) __attribute__((always_inline)) {  // of a stage: all but the last
 #pragma unroll
@@ -477,14 +486,14 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
             }
         };
         auto on = [&]() __attribute__((always_inline)) {
-            stage += T::STAGE;
-            if (stage == stages + T::NS * T::STAGE) stage = stages;
+            stage += STAGE;
+            if (stage == stages + NS * STAGE) stage = stages;
         };
         read(stage, 0, f0);
         first_steps(std::false_type{});
         int kt = 1;
-        for (; kt <= nk - T::NS; ++kt) {  // (T::NS - 2 stages are in flight behind this one)
-            landed(kt, T::NS - 2);
+        for (; kt <= nk - NS; ++kt) {
+            landed(kt, NS - 2);
             on();
             begin_stage();
             step(stage, 0, f0, f1, std::true_type{}, 0);
@@ -492,7 +501,7 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
             end_stage();
         }
         for (; kt < nk; ++kt) {
-            landed(kt, min(nk - 1 - kt, T::NS - 2));
+            landed(kt, min(nk - 1 - kt, NS - 2));
             on();
             step(stage, 0, f0, f1, std::false_type{}, 0);
             first_steps(std::false_type{});
@@ -507,9 +516,20 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
     };
 
     // ---- out.  The matrix cores leave lane l of a block with row l & 31 and columns 8 q + 4 (l >> 5) + 0..3, q = 0..3: 16 bytes of fp32, but 8 of
-    // bf16, where the halves of a wavefront swap what they have of two q, so that lanes below 32 have 16 bytes of one and the others of the other.
+    // bf16, where the halves of a wavefront swap what they have of two q, so that the lower one has 16 bytes of one and the upper one of the
+    // other.  Then lanes of 16 to 31 and of 0 to 15 swap, so that an access reaches 64 bytes of each of 16 rows: piece 2 j + i of a lane is
+    // row 16 i + (l & 15), columns (4 j + 2 (l >> 4 & 1) + (l >> 5)) * PIECE and on.
     constexpr int COL_BLOCKS = GATED ? T::NB / 2 : T::NB;
     constexpr int PIECES = 32 * SZ / 32;  // pieces of 16 bytes that a lane has of a block: 2 of bf16, 4 of fp32
+    auto swap16 = [&](u32x4_t (&v)[PIECES]) __attribute__((always_inline)) {  // (its own inverse)
+#pragma unroll
+        for (int i = 0; i < PIECES; i += 2)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const auto x = __builtin_amdgcn_permlane16_swap(v[i][j], v[i + 1][j], false, false);
+                v[i][j] = x[0], v[i + 1][j] = x[1];
+            }
+    };
     auto pieces_of = [&](auto value, u32x4_t (&v)[PIECES]) __attribute__((always_inline)) {  // value(register)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -525,8 +545,10 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
                 for (int j = 0; j < 4; ++j) v[i][j] = __float_as_uint(value(4 * i + j));
             }
         }
+        swap16(v);
     };
-    auto values_of = [&](const u32x4_t (&v)[PIECES], float (&x)[16]) __attribute__((always_inline)) {  // the other way
+    auto values_of = [&](u32x4_t (&v)[PIECES], float (&x)[16]) __attribute__((always_inline)) {  // the other way
+        swap16(v);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             if constexpr (SZ == 2) {
@@ -542,32 +564,55 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
             }
         }
     };
-    auto write_tile = [&](const Tile &w) __attribute__((always_inline)) {
+    // Where a lane's pieces of block (mb, nb) of a tile are; f(number of the piece, row of the segment or matrix, column) for those there are.
+    auto each_piece = [&](const Tile &w, int mb, int nb, int l, auto f) __attribute__((always_inline)) {
+        const int m = w.row0 + (mb * T::WM + wm) * 32 + (l & 15), n = w.n0 + (wn * COL_BLOCKS + nb) * 32 + ((l >> 4 & 1) * 2 + (l >> 5)) * PIECE;
         const int rows = DW ? a.M : w.s.extent;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (m + i % 2 * 16 < rows && n + i / 2 * 4 * PIECE < a.N) f(i, m + i % 2 * 16, n + i / 2 * 4 * PIECE);
+    };
+    auto there = [&](const Tile &w, int mb, int nb) __attribute__((always_inline)) {  // any of the block
+        return w.n0 + (wn * COL_BLOCKS + nb) * 32 < a.N && w.row0 + (mb * T::WM + wm) * 32 < (DW ? a.M : w.s.extent);
+    };
+    // dh: g and u of the blocks, GU_AHEAD ahead of the one that takes them
+    constexpr int BLOCKS = T::MB * COL_BLOCKS, GU_AHEAD = OP != kFfnDh ? 0 : BLOCKS < (SZ == 2 ? 6 : 2) ? BLOCKS : (SZ == 2 ? 6 : 2);
+    u32x4_t gv[GU_AHEAD + 1][PIECES], uv[GU_AHEAD + 1][PIECES];
+    auto load_gu = [&](const Tile &w, int block) __attribute__((always_inline)) {
+        const int mb = block / COL_BLOCKS, nb = block % COL_BLOCKS, at = block % (GU_AHEAD + (OP != kFfnDh));
+        if (!there(w, mb, nb)) return;
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        each_piece(w, mb, nb, l, [&](int i, int m, int n) __attribute__((always_inline)) {
+            const size_t from = (size_t)(w.s.begin + m) * a.ldg + n;
+            gv[at][i] = *(const u32x4_t *)((const ET *)a.g + from), uv[at][i] = *(const u32x4_t *)((const ET *)a.u + from);
+        });
+    };
+    auto write_tile = [&](const Tile &w) __attribute__((always_inline)) {
 #pragma unroll
         for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
             for (int nb = 0; nb < COL_BLOCKS; ++nb) {
                 __builtin_amdgcn_sched_barrier(0);  // (results of one block at a time: registers)
-                const int m0 = w.row0 + (wm * T::MB + mb) * 32, n0 = w.n0 + (wn * COL_BLOCKS + nb) * 32;
-                if (n0 >= a.N || m0 >= rows) continue;
+                constexpr int GU = GU_AHEAD ? GU_AHEAD : 1;
+                const int block = mb * COL_BLOCKS + nb;
+                if (!there(w, mb, nb)) {
+                    if (OP == kFfnDh && a.o0 && block + GU < BLOCKS) load_gu(w, block + GU);
+                    continue;
+                }
                 // (or the places and sums of all blocks are fetched ahead into vector registers, and spilled)
                 int l = lane;
                 asm volatile("" : "+v"(l));
                 asm volatile("" : "+a"(acc[mb][nb]));
                 if (GATED) asm volatile("" : "+a"(acc[mb][nb + T::NB / 2]));
-                const int m = m0 + (l & 31), n = n0 + (l >> 5) * PIECE;  // and 2 * PIECE columns further from piece to piece
-                const bool in = m < rows, used = DW || m < w.s.used;
-                const size_t row = (DW ? 0 : (size_t)w.s.begin) + m;
+                const size_t first = DW ? 0 : (size_t)w.s.begin;
                 auto put = [&](auto value, void *to, long long ld) __attribute__((always_inline)) {
                     u32x4_t v[PIECES];
                     pieces_of(value, v);
-                    u32x4_t *p = (u32x4_t *)((ET *)to + row * ld + n);
-#pragma unroll
-                    for (int i = 0; i < PIECES; ++i) {
-                        if (!used) v[i] = u32x4_t{0, 0, 0, 0};  // (an unused row has the sums of a used one)
-                        if (in && n + 2 * PIECE * i < a.N) p[2 * i] = v[i];
-                    }
+                    each_piece(w, mb, nb, l, [&](int i, int m, int n) __attribute__((always_inline)) {
+                        if (!DW && m >= w.s.used) v[i] = u32x4_t{0, 0, 0, 0};  // (an unused row has the sums of a used one)
+                        *(u32x4_t *)((ET *)to + (first + m) * ld + n) = v[i];
+                    });
                 };
                 auto sum = [&](int i) __attribute__((always_inline)) { return acc[mb][nb][i]; };
                 if constexpr (OP == kFfnUp) {
@@ -577,17 +622,11 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
                 } else if constexpr (OP == kFfnDh) {
                     if (a.o2) put(sum, a.o2, a.N);
                     if (!a.o0) continue;
-                    u32x4_t v[PIECES], w[PIECES];
-                    const size_t at = row * a.ldg + n;
-#pragma unroll
-                    for (int i = 0; i < PIECES; ++i) {
-                        v[i] = w[i] = u32x4_t{0, 0, 0, 0};
-                        if (in && n + 2 * PIECE * i < a.N)
-                            v[i] = *(const u32x4_t *)((const ET *)a.g + at + 2 * PIECE * i), w[i] = *(const u32x4_t *)((const ET *)a.u + at + 2 * PIECE * i);
-                    }
+                    const int at = block % GU;
                     float g[16], u[16];
-                    values_of(v, g);
-                    values_of(w, u);
+                    values_of(gv[at], g);
+                    values_of(uv[at], u);
+                    if (block + GU < BLOCKS) load_gu(w, block + GU);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float s = sigmoid<ET>(g[i]);
@@ -634,6 +673,12 @@ __global__ __launch_bounds__(T::THREADS) void k_ffn(FfnArgs a) {
             __syncthreads();  // (everybody has read the answer before)
             answer();
             __syncthreads();
+        }
+        if constexpr (OP == kFfnDh) {
+            if (a.o0) {
+#pragma unroll
+                for (int i = 0; i < GU_AHEAD; ++i) load_gu(now, i);
+            }
         }
         if (a.plan)
             tile = uniform(tables->next);

@@ -53,7 +53,7 @@ static int prepare(FfnArgs &a, Launch *l) {
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
     if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
-    const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * (160 * 1024 / T::SMEM);
+    const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * T::OCC;
     l->kernel = (const void *)k_ffn<T, OP>;
     l->groups = (unsigned)(tiles < room ? tiles : room);
     l->smem = T::SMEM;
@@ -65,16 +65,16 @@ static int prepare(FfnArgs &a, Launch *l) {
 template <typename ET, FfnOp OP>
 static int pick(FfnArgs &a, int slots, Launch *l) {
     if constexpr (sizeof(ET) == 4) {
-        return slots / a.E > 48 ? prepare<FfnTile<ET, 2, 2, 2, 2, 64, 4>, OP>(a, l) : prepare<FfnTile<ET, 1, 2, 1, 4, 64, 4>, OP>(a, l);
+        return slots / a.E > 48 ? prepare<FfnTile<ET, 2, 2, 2, 2, 64, 2>, OP>(a, l) : prepare<FfnTile<ET, 1, 2, 1, 4, 64, 2>, OP>(a, l);
     } else {
 #ifndef V256
-#define V256 8, 2, 1, 4, 64, 4
+#define V256 4, 4, 2, 2, 64, 1
 #endif
 #ifndef V128
-#define V128 2, 4, 2, 2, 64, 4
+#define V128 4, 4, 2, 2, 64, 1
 #endif
 #ifndef V32
-#define V32 1, 2, 1, 4, 128, 3
+#define V32 1, 2, 1, 4, 128, 1
 #endif
         if (slots / a.E > 160) return prepare<FfnTile<ET, V256>, OP>(a, l);
         return slots / a.E > 48 ? prepare<FfnTile<ET, V128>, OP>(a, l) : prepare<FfnTile<ET, V32>, OP>(a, l);
@@ -83,10 +83,10 @@ static int pick(FfnArgs &a, int slots, Launch *l) {
 template <typename ET>
 static int pick_dw(FfnArgs &a, Launch *l) {
     if constexpr (sizeof(ET) == 4)
-        return prepare<FfnTile<ET, 2, 2, 2, 2, 64, 4>, kFfnDw>(a, l);
+        return prepare<FfnTile<ET, 2, 2, 2, 2, 64, 2>, kFfnDw>(a, l);
     else
 #ifndef VDW
-#define VDW 4, 4, 2, 2, 64, 4
+#define VDW 4, 4, 2, 2, 64, 1
 #endif
         return prepare<FfnTile<ET, VDW>, kFfnDw>(a, l);
 }
