@@ -26,12 +26,15 @@ struct FfnArgs {
     int E, rows, capacity;
     const int32_t *counts;
     int M, N, K;     // N columns per matrix; K reduction steps per pair of operands; dw: M x N per matrix, reduction over the rows
+    bool down;       // dw: it is dW2
     int mt, nt;      // column tiles of all matrices; dw: row tiles
     long long lda, ldb, ldo, ldg;  // elements from one row to the next: operands, outputs, g and u
     long long eb, eo;              // elements from one expert's matrix to the next: weights; dw: outputs
     const void *A0, *A1, *B0, *B1;
     const void *g, *u;  // dh: the activation's inputs
     void *o0, *o1, *o2;
+    int split;    // parts that the reduction is cut into; their sums go to `part`, and k_ffn_join makes the outputs of them
+    float *part;  // [split][rows][N] (up: g then u for each part); dw: [split][matrix][E][M][N]
     const struct FfnPlan *plan;  // of k_ffn_plan, NULL: every workgroup makes its own tables and takes every n-th tile
 };
 
@@ -84,12 +87,12 @@ struct FfnPlan {
     mutable Counter taken[kTileQueues];  // tiles handed out of an XCD's list, beyond the first ones
 };
 
-// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts (row blocks go round those of a column), stages of KB bytes of the reduction, as
-// many as fit the LDS of OCC workgroups per CU.
-template <typename ET_, int MB_, int NB_, int WM_, int WN_, int KB_, int OCC_>
+// MB x NB blocks of 32 x 32 per wavefront, WM x WN wavefronts (row blocks go round those of a column) and KW of each, which share a stage's steps;
+// stages of KB bytes of the reduction, as many as fit the LDS of OCC workgroups per CU.
+template <typename ET_, int MB_, int NB_, int WM_, int WN_, int KW_, int KB_, int OCC_>
 struct FfnTile {
     typedef ET_ ET;
-    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KB = KB_, OCC = OCC_, WAVES = WM * WN;
+    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, KW = KW_, KB = KB_, OCC = OCC_, WAVES = WM * WN * KW;
     static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN;
     static constexpr int ROOM = (160 * 1024 / OCC - (int)sizeof(FfnTables)) / 1024 * 1024, SMEM = ROOM + (int)sizeof(FfnTables);
     static constexpr int stage_bytes(int live) { return (BN + BM / MB * live) * KB; }  // of a tile with `live` row blocks per wavefront
@@ -138,24 +141,40 @@ __device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables 
     const int tid = threadIdx.x;
     static_assert(kThreads >= kMaxExperts, "a thread per expert");
     const int n = tid < a.E ? min(max(a.counts[tid], 0), a.rows) : 0;
-    int begin, used, blocks;
+    int begin = tid * a.capacity, used = min(n, a.capacity), first, total, last = a.rows;
     u64 all;
     if (a.capacity) {
-        begin = tid * a.capacity, used = min(n, a.capacity), blocks = (a.capacity + bm - 1) / bm;
-    } else {
-        const u64 end = scan_workgroup((u64)n, t->sum, &all);
-        begin = (int)min(end - n, (u64)a.rows), used = (int)min(end, (u64)a.rows) - begin, blocks = (used + bm - 1) / bm;
-        if (tid == 0) t->begin[a.E] = (int)min(all, (u64)a.rows);
-    }
-    if (DW) blocks = used + kDwStart;
-    if (tid >= a.E) blocks = 0;
-    const int to = (int)scan_workgroup((u64)blocks, t->sum + 4, &all);
-    if (tid < a.E) t->begin[tid] = begin, t->used[tid] = used, t->first[tid] = to - blocks;
-    if (tid == 0) t->first[a.E] = (int)all;
-    __syncthreads();
-    const int total = (int)all;
-    if (tid <= kTileQueues) {
         if (DW) {
+            const int to = (int)scan_workgroup((u64)(tid < a.E ? used + kDwStart : 0), t->sum, &all);
+            first = to - used - kDwStart, total = (int)all;
+        } else {
+            const int blocks = (a.capacity + bm - 1) / bm;
+            first = tid * blocks, total = a.E * blocks;
+        }
+    } else {
+        // rows and blocks in one scan, 39 and 25 bits
+        constexpr u64 kRows = ((u64)1 << 39) - 1;
+        const u64 end = scan_workgroup((u64)((n + bm - 1) / bm) << 39 | (u64)n, t->sum, &all), rows_end = end & kRows;
+        last = (int)min(all & kRows, (u64)a.rows);
+        begin = (int)min(rows_end - n, (u64)a.rows), used = (int)min(rows_end, (u64)a.rows) - begin;
+        if (DW) {
+            first = begin + tid * kDwStart, total = last + a.E * kDwStart;
+        } else if ((all & kRows) <= (u64)a.rows && a.rows <= 1 << 29) {
+            first = (int)(end >> 39) - (n + bm - 1) / bm, total = (int)(all >> 39);
+        } else {  // counts that are cut, or more blocks than 25 bits hold
+            const int blocks = (used + bm - 1) / bm;
+            first = (int)scan_workgroup((u64)blocks, t->sum + 4, &all) - blocks, total = (int)all;
+        }
+    }
+    if (tid < a.E) t->begin[tid] = begin, t->used[tid] = used, t->first[tid] = first;
+    if (tid == 0) t->begin[a.E] = last, t->first[a.E] = total;
+    if (!DW && tid <= kTileQueues) {
+        const int row_blocks = total + (a.capacity ? 0 : (a.rows - last + bm - 1) / bm);
+        t->edge[tid] = (int)((i64)row_blocks * a.nt * tid / kTileQueues);
+    }
+    __syncthreads();
+    if (DW) {
+        if (tid <= kTileQueues) {
             // stretches of about the same work: a tile is worth its expert's rows and kDwStart
             const int per = a.mt * a.nt;
             const u64 at = (u64)tid * (u32)total;
@@ -163,12 +182,9 @@ __device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables 
             for (int step = kMaxExperts / 2; step; step >>= 1)
                 if (e + step < a.E && t->first[e + step] <= (int)(at / kTileQueues)) e += step;
             t->edge[tid] = tid == kTileQueues ? a.E * per : e * per + (int)((at - (u64)kTileQueues * t->first[e]) * per / (u64)(kTileQueues * (t->used[e] + kDwStart)));
-        } else {
-            const int row_blocks = total + (a.capacity ? 0 : (a.rows - t->begin[a.E] + bm - 1) / bm);
-            t->edge[tid] = (int)((i64)row_blocks * a.nt * tid / kTileQueues);
         }
+        __syncthreads();
     }
-    __syncthreads();
 }
 
 // One workgroup makes the tables for the launch or two that follow.
@@ -238,6 +254,27 @@ __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32
     }
 }
 
+// Eight fp32 numbers as three bf16 numbers each, x = p0 + p1 + p2 with |p1| <= 2^-9 |x| and |p2| <= 2^-18 |x|, off by 2^-27 |x| at most.  Of
+// the nine products of two numbers the six largest are taken; the others come to 2^-26 of the whole.  On the matrix cores those six take 192 cycles
+// for 32 x 32 x 16, the fp32 instructions 512.  A number that is not finite, or that bf16 rounds to one, makes a NaN of every sum that it is in.
+struct Cut {
+    u32x4_t part[3];
+};
+__device__ __forceinline__ Cut cut_f32(const u32x4_t &lo, const u32x4_t &hi) {
+    Cut c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x = __uint_as_float(i < 2 ? lo[2 * i] : hi[2 * i - 4]), y = __uint_as_float(i < 2 ? lo[2 * i + 1] : hi[2 * i - 3]);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const u32 p = pack_bf16x2(x, y);
+            c.part[j][i] = p;
+            x -= __uint_as_float(p << 16), y -= __uint_as_float(p & 0xffff0000u);
+        }
+    }
+    return c;
+}
+
 template <class T, FfnOp OP>
 __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     typedef typename T::ET ET;
@@ -250,7 +287,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     extern __shared__ __align__(128) char smem[];
     char *stages = smem;
     FfnTables *tables = (FfnTables *)(smem + T::ROOM);
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % T::WN, wm = wave / T::WN % T::WM, wk = wave / (T::WN * T::WM);
     if (a.plan) {
         for (int i = tid; i < (int)(sizeof(FfnTables) / 4); i += kThreads) ((u32 *)tables)[i] = ((const u32 *)&a.plan->tables)[i];
         __syncthreads();
@@ -289,7 +326,8 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     const int per_matrix = (a.N + COLS - 1) / COLS;  // dw: column tiles of the second matrix lie behind those of the first
     struct Tile {
         Segment s;
-        int row0, n0, matrix, nk;  // first row (of the segment's; dw: of the matrix) and column, stages
+        int row0, n0, matrix;  // first row (of the segment's; dw: of the matrix) and column
+        int part, k0, nk, end;  // part of the reduction: its first stage and how many; stages of the whole
     };
     auto tile_at = [&](int t) __attribute__((always_inline)) {
         Tile w;
@@ -300,7 +338,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             tile_in_groups(t - w.s.e * per, a.mt, a.nt, &r, &c);
             w.s.begin = uniform(tables->begin[w.s.e]), w.s.used = w.s.extent = uniform(tables->used[w.s.e]);
             w.row0 = r * T::BM;
-            w.nk = (w.s.used + STEPS - 1) / STEPS;
+            w.end = (w.s.used + STEPS - 1) / STEPS;
         } else {
             tile_in_groups(t, row_blocks, a.nt, &r, &c);
             const int e = last_up_to(tables->first, a.E + 1, r);
@@ -309,15 +347,17 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             w.s.used = e < a.E ? uniform(tables->used[e]) : 0;
             w.s.extent = a.capacity ? a.capacity : e < a.E ? w.s.used : a.rows - w.s.begin;
             w.row0 = w.s.block * T::BM;
-            w.nk = w.row0 >= w.s.used ? 0 : OP == kFfnDx ? 2 * half : half;
+            w.end = w.row0 >= w.s.used ? 0 : OP == kFfnDx ? 2 * half : half;
         }
+        w.part = c % a.split, c /= a.split;
+        w.k0 = (int)((i64)w.end * w.part / a.split), w.nk = (int)((i64)w.end * (w.part + 1) / a.split) - w.k0;
         w.matrix = DW ? c / per_matrix : 0;
         w.n0 = (c - w.matrix * per_matrix) * COLS;
         return w;
     };
 
     // Row blocks that are not full have loops of their own, for a quarter, a half and three quarters of the rows, and more stages in flight.
-    constexpr bool SHORT = !DW && T::MB % 4 == 0;
+    constexpr bool SHORT = !DW && SZ == 2 && T::MB % 4 == 0;
     auto loads_of_a = [](int live) __attribute__((always_inline)) { return (OA::INSTR * live / T::MB + T::WAVES - 1) / T::WAVES; };
 
     // ---- loads.  A lane's places in the operands; they go on from stage to stage.
@@ -325,20 +365,20 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     const size_t lda = (size_t)a.lda * SZ, ldb = (size_t)a.ldb * SZ;
     const size_t a_step = AK ? T::KB : STEPS * lda, b_step = BK ? T::KB : STEPS * ldb;
     const u32 lds = lds_offset(stages);
-    int next, nk, used;  // the stage to load; stages and rows of the tile that is loaded
+    int next, k0, nk, end, used;  // the stage to load; stages and rows of the tile that is loaded
     int live, a_loads;   // row blocks per wavefront it has, loads of A per wavefront
     u32 stage_bytes, to_end;
     u32 to;              // where it goes
     // before a stage's loads: on to the second pair of operands; rows past the expert's last one are that one again
     auto begin_stage = [&]() __attribute__((always_inline)) {
-        if (OP == kFfnDx && next == half) {
+        if (OP == kFfnDx && next == half && k0 < half) {
             const long long da = (const char *)a.A1 - (const char *)a.A0 - (long long)half * T::KB, db = (const char *)a.B1 - (const char *)a.B0 - (long long)half * T::KB;
 #pragma unroll
             for (int i = 0; i < OA::PER_WAVE; ++i) ap[i] += da;
 #pragma unroll
             for (int i = 0; i < OB::PER_WAVE; ++i) bp[i] += db;
         }
-        if (OP == kFfnDw && next == nk - 1) {
+        if (OP == kFfnDw && next == end - 1) {
             const int left = used - 1 - next * STEPS;
 #pragma unroll
             for (int i = 0; i < OA::PER_WAVE; ++i) ap[i] -= (size_t)max(OA::row_of(OA::instr(wave, i), lane) - left, 0) * lda;
@@ -373,14 +413,16 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     };
     // The first stages of a tile: nobody may be reading the stages any more.
     auto start = [&](const Tile &w) __attribute__((always_inline)) {
-        nk = w.nk, used = w.s.used, next = 0, to = lds;
+        next = k0 = w.k0, nk = w.nk, end = w.end, used = w.s.used, to = lds;
         if (!nk) return;
         const int rows = used - w.row0;
         live = !SHORT || rows > T::BM / 4 * 3 ? T::MB : rows > T::BM / 2 ? T::MB / 4 * 3 : rows > T::BM / 4 ? T::MB / 2 : T::MB / 4;
         a_loads = loads_of_a(live), stage_bytes = T::stage_bytes(live);
         const int ns = live == T::MB ? T::stages(T::MB) : live == T::MB / 4 * 3 ? T::stages(T::MB / 4 * 3) : live == T::MB / 2 ? T::stages(T::MB / 2) : T::stages(T::MB / 4);
         to_end = lds + ns * stage_bytes;
-        const char *A = (const char *)a.A0, *B = (const char *)(DW && w.matrix ? a.B1 : a.B0);
+        const bool second = OP == kFfnDx && k0 >= half;  // of the pairs of operands
+        const char *A = (const char *)(second ? a.A1 : a.A0) + (size_t)(second ? k0 - half : k0) * a_step;
+        const char *B = (const char *)((DW && w.matrix) || second ? a.B1 : a.B0) + (size_t)(second ? k0 - half : k0) * b_step;
 #pragma unroll
         for (int i = 0; i < OA::PER_WAVE; ++i) {
             const int in = OA::instr(wave, i), r = OA::row_of(in, lane), c = OA::piece_of(in, lane);
@@ -399,7 +441,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             } else {
                 int n = c * PIECE;
                 const char *from = B;
-                if (GATED && n >= COLS) from = (const char *)a.B1, n -= COLS;
+                if (GATED && n >= COLS) from += (const char *)a.B1 - (const char *)a.B0, n -= COLS;
                 n += w.n0;
                 const size_t first = DW ? (size_t)w.s.begin * ldb : (size_t)w.s.e * a.eb * SZ;
                 bp[i] = from + first + (size_t)r * ldb + (size_t)(n < a.N ? n : 0) * SZ;
@@ -420,9 +462,10 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
 
     // Fragments are read a step ahead of the products that take them; a stage's buffer is free when everybody has read its last
     // fragments, and the loads of the stage that goes there are dealt out over the steps that follow.
-    constexpr int KK = T::KB / 32;  // steps per stage
+    constexpr int KK = T::KB / 32 / T::KW;  // a wavefront's steps per stage
     static_assert(KK % 2 == 0, "two sets of fragments in turn");
-    auto products = [&](auto blocks) __attribute__((always_inline)) {
+    auto products = [&](auto blocks, auto cut) __attribute__((always_inline)) {
+        constexpr bool CUT = decltype(cut)::value, ASK = SZ == 2 || CUT;  // (once per tile)
         constexpr int LIVE = decltype(blocks)::value, NS = T::stages(LIVE), STAGE = T::stage_bytes(LIVE);
         static_assert(NS >= 2, "stages");
         constexpr int AL = (OA::INSTR * LIVE / T::MB + T::WAVES - 1) / T::WAVES, LPS = AL + OB::PER_WAVE;  // loads per wavefront and stage
@@ -433,8 +476,8 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         };
         Frags f0, f1;
         auto read = [&](const char *stage, int kk, Frags &f) __attribute__((always_inline)) {
-            read_frags<OA>(stage + OB::BYTES, kk, a_at, lane, f.a);
-            read_frags<OB>(stage, kk, b_at, lane, f.b);
+            read_frags<OA>(stage + OB::BYTES, wk * KK + kk, a_at, lane, f.a);
+            read_frags<OB>(stage, wk * KK + kk, b_at, lane, f.b);
         };
         // products of `cur`, with the reads of `nxt` and, if LOADS, share `part` of a stage's loads in between
         auto step = [&](const char *stage, int kk, Frags &nxt, const Frags &cur, auto loads, int part) __attribute__((always_inline)) {
@@ -464,7 +507,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             wait_behind<NS - 1, LPS>(behind);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
-            if (OP == kFfnDw && kt == nk - 1 && used % STEPS) {
+            if (OP == kFfnDw && k0 + kt == end - 1 && used % STEPS) {
                 // the steps past the expert's last row: zeros in both operands, whatever lies there
                 char *stage = stages + kt % NS * STAGE;
                 const int from = used % STEPS;
@@ -489,29 +532,87 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             stage += STAGE;
             if (stage == stages + NS * STAGE) stage = stages;
         };
-        read(stage, 0, f0);
-        first_steps(std::false_type{});
-        int kt = 1;
-        for (; kt <= nk - NS; ++kt) {
-            landed(kt, NS - 2);
-            on();
-            begin_stage();
-            step(stage, 0, f0, f1, std::true_type{}, 0);
-            first_steps(std::true_type{});
-            end_stage();
-        }
-        for (; kt < nk; ++kt) {
-            landed(kt, min(nk - 1 - kt, NS - 2));
-            on();
-            step(stage, 0, f0, f1, std::false_type{}, 0);
+        if constexpr (CUT) {
+            // (two workgroups per CU: while one reads and cuts, the other multiplies)
+            Cut ca[LIVE], cb[T::NB];
+            auto read_cut = [&]() __attribute__((always_inline)) {
+                Frags lo, hi;
+                read(stage, 0, lo);
+                read(stage, 1, hi);
+#pragma unroll
+                for (int i = 0; i < LIVE; ++i) ca[i] = cut_f32(lo.a[i], hi.a[i]);
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i) cb[i] = cut_f32(lo.b[i], hi.b[i]);
+            };
+            auto multiply_cut = [&]() __attribute__((always_inline)) {
+                constexpr int kTerms[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};  // (the smallest first)
+#pragma unroll
+                for (int t = 0; t < 6; ++t)
+#pragma unroll
+                    for (int mb = 0; mb < LIVE; ++mb)
+#pragma unroll
+                        for (int nb = 0; nb < T::NB; ++nb) multiply<bf16_t>(cb[nb].part[kTerms[t][1]], ca[mb].part[kTerms[t][0]], acc[mb][nb]);
+            };
+            read_cut();
+            for (int kt = 1; kt < nk; ++kt) {
+                multiply_cut();
+                landed(kt, min(nk - 1 - kt, NS - 2));
+                on();
+                if (next < k0 + nk) load_stage();
+                read_cut();
+            }
+            if (ASK) ask();
+            multiply_cut();
+        } else {
+            read(stage, 0, f0);
             first_steps(std::false_type{});
+            int kt = 1;
+            for (; kt <= nk - NS; ++kt) {
+                landed(kt, NS - 2);
+                on();
+                begin_stage();
+                step(stage, 0, f0, f1, std::true_type{}, 0);
+                first_steps(std::true_type{});
+                end_stage();
+            }
+            for (; kt < nk; ++kt) {
+                landed(kt, min(nk - 1 - kt, NS - 2));
+                on();
+                step(stage, 0, f0, f1, std::false_type{}, 0);
+                first_steps(std::false_type{});
+            }
+            if (ASK) ask();  // (no load is in flight any more: the wait for the answer holds nothing up)
+#pragma unroll
+            for (int mb = 0; mb < LIVE; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(f1.b[nb], f1.a[mb], acc[mb][nb]);
         }
-        ask();  // (no load is in flight any more: the wait for the answer holds nothing up)
+        if constexpr (T::KW > 1) {  // the sums of the wavefronts that shared the steps meet with the first one's
+            static_assert(T::KW == 2 && 2 * T::WM * T::WN * T::MB * T::NB * 2048 <= T::ROOM, "two of them");
+            __syncthreads();
+            f32x4_t *x = (f32x4_t *)stages + (wave % (T::WM * T::WN)) * T::MB * T::NB * 256 + lane;
 #pragma unroll
-        for (int mb = 0; mb < LIVE; ++mb)
+            for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) multiply<ET>(f1.b[nb], f1.a[mb], acc[mb][nb]);
-        answer();
+                for (int nb = 0; nb < T::NB; ++nb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16_t &v = acc[mb][nb];
+                        if (wk) x[((mb * T::NB + nb) * 4 + q) * 64] = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    }
+            __syncthreads();
+#pragma unroll
+            for (int mb = 0; mb < T::MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4_t v = x[((mb * T::NB + nb) * 4 + q) * 64];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[mb][nb][4 * q + j] += v[j];
+                    }
+        }
+        if (ASK) answer();
         __syncthreads();
     };
 
@@ -576,7 +677,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         return w.n0 + (wn * COL_BLOCKS + nb) * 32 < a.N && w.row0 + (mb * T::WM + wm) * 32 < (DW ? a.M : w.s.extent);
     };
     // dh: g and u of the blocks, GU_AHEAD ahead of the one that takes them
-    constexpr int BLOCKS = T::MB * COL_BLOCKS, GU_AHEAD = OP != kFfnDh ? 0 : BLOCKS < (SZ == 2 ? 6 : 2) ? BLOCKS : (SZ == 2 ? 6 : 2);
+    constexpr int BLOCKS = T::MB * COL_BLOCKS, GU_MOST = SZ == 4 ? 1 : T::OCC == 1 ? 6 : 3, GU_AHEAD = OP != kFfnDh ? 0 : BLOCKS < GU_MOST ? BLOCKS : GU_MOST;
     u32x4_t gv[GU_AHEAD + 1][PIECES], uv[GU_AHEAD + 1][PIECES];
     auto load_gu = [&](const Tile &w, int block) __attribute__((always_inline)) {
         const int mb = block / COL_BLOCKS, nb = block % COL_BLOCKS, at = block % (GU_AHEAD + (OP != kFfnDh));
@@ -589,6 +690,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         });
     };
     auto write_tile = [&](const Tile &w) __attribute__((always_inline)) {
+        if (T::KW > 1 && wk) return;
 #pragma unroll
         for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
@@ -597,7 +699,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
                 constexpr int GU = GU_AHEAD ? GU_AHEAD : 1;
                 const int block = mb * COL_BLOCKS + nb;
                 if (!there(w, mb, nb)) {
-                    if (OP == kFfnDh && a.o0 && block + GU < BLOCKS) load_gu(w, block + GU);
+                    if (OP == kFfnDh && a.o0 && a.split == 1 && block + GU < BLOCKS) load_gu(w, block + GU);
                     continue;
                 }
                 // (or the places and sums of all blocks are fetched ahead into vector registers, and spilled)
@@ -606,6 +708,20 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
                 asm volatile("" : "+a"(acc[mb][nb]));
                 if (GATED) asm volatile("" : "+a"(acc[mb][nb + T::NB / 2]));
                 const size_t first = DW ? 0 : (size_t)w.s.begin;
+                if (a.split > 1) {  // the sums themselves: 4 columns of a row at a time
+#pragma unroll
+                    for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+                        const f32x16_t &v = acc[mb][nb + h * (GATED ? T::NB / 2 : 0)];
+                        const int m = w.row0 + (mb * T::WM + wm) * 32 + (l & 31), n = w.n0 + (wn * COL_BLOCKS + nb) * 32 + (l >> 5) * 4;
+                        const size_t row = DW ? ((size_t)w.part * (a.o1 ? 2 : 1) + w.matrix) * a.E * a.M + (size_t)w.s.e * a.M + m
+                                              : ((size_t)w.part * (GATED ? 2 : 1) + h) * a.rows + first + m;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (m < (DW ? a.M : w.s.used) && n + 8 * q < a.N)
+                                *(f32x4_t *)(a.part + row * a.N + n + 8 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    }
+                    continue;
+                }
                 auto put = [&](auto value, void *to, long long ld) __attribute__((always_inline)) {
                     u32x4_t v[PIECES];
                     pieces_of(value, v);
@@ -647,25 +763,43 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     // The next tile's first stages are on their way while this one's results go out.
     Tile now = tile_at(tile);
     start(now);
-    while (true) {
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
             for (int nb = 0; nb < T::NB; ++nb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[mb][nb][v] = 0.f;
+    };
+    while (true) {
+        clear();
         if (nk) {
+            auto run = [&](auto blocks) __attribute__((always_inline)) { products(blocks, std::integral_constant<bool, SZ == 4>{}); };
             if constexpr (SHORT) {
                 if (live == T::MB)
-                    products(std::integral_constant<int, T::MB>{});
+                    run(std::integral_constant<int, T::MB>{});
                 else if (live == T::MB / 4 * 3)
-                    products(std::integral_constant<int, T::MB / 4 * 3>{});
+                    run(std::integral_constant<int, T::MB / 4 * 3>{});
                 else if (live == T::MB / 2)
-                    products(std::integral_constant<int, T::MB / 2>{});
+                    run(std::integral_constant<int, T::MB / 2>{});
                 else
-                    products(std::integral_constant<int, T::MB / 4>{});
+                    run(std::integral_constant<int, T::MB / 4>{});
             } else {
-                products(std::integral_constant<int, T::MB>{});
+                run(std::integral_constant<int, T::MB>{});
+            }
+            if constexpr (SZ == 4) {  // with numbers that are not finite again, on the fp32 instructions
+                bool bad = false;
+#pragma unroll
+                for (int mb = 0; mb < T::MB; ++mb)
+#pragma unroll
+                    for (int nb = 0; nb < T::NB; ++nb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) bad |= acc[mb][nb][v] != acc[mb][nb][v];
+                if (__syncthreads_or(bad)) {
+                    clear();
+                    start(now);
+                    products(std::integral_constant<int, T::MB>{}, std::false_type{});
+                }
             }
         }
         else {
@@ -675,7 +809,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             __syncthreads();
         }
         if constexpr (OP == kFfnDh) {
-            if (a.o0) {
+            if (a.o0 && a.split == 1) {
 #pragma unroll
                 for (int i = 0; i < GU_AHEAD; ++i) load_gu(now, i);
             }
@@ -688,6 +822,84 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         if (tile >= 0) now = tile_at(tile), start(now);
         write_tile(done);
         if (tile < 0) break;
+    }
+}
+
+// The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.
+template <typename ET, FfnOp OP>
+__global__ __launch_bounds__(kThreads) void k_ffn_join(FfnArgs a) {
+    __shared__ u64 lds[8];
+    constexpr bool DW = OP == kFfnDw;
+    const int tid = threadIdx.x, cols = a.N / 8;
+    int last = 0;  // ragged: the rows that are anybody's
+    if (!DW && !a.capacity) {
+        u64 all;
+        scan_workgroup((u64)(tid < a.E ? min(max(a.counts[tid], 0), a.rows) : 0), lds, &all);
+        last = (int)min(all, (u64)a.rows);
+    }
+    const size_t rows = DW ? (size_t)a.E * a.M : a.rows, mats = DW ? (a.o1 ? 2 : 1) : 1;
+    const size_t part = rows * a.N * (OP == kFfnUp ? 2 : mats);
+    for (size_t i = (size_t)blockIdx.x * kThreads + tid; i < rows * mats * cols; i += (size_t)gridDim.x * kThreads) {
+        const size_t r = i / cols;
+        const int n = (int)(i - r * cols) * 8;
+        const size_t matrix = r / rows, row = r - matrix * rows;
+        bool used = true;
+        if (!DW) {
+            const int e = a.capacity ? (int)(row / a.capacity) : 0;
+            used = a.capacity ? (int)row - e * a.capacity < a.counts[e] : (int)row < last;
+        }
+        float v[8] = {}, w[8] = {};
+        if (used) {
+            const float *p = a.part + r * a.N + n;
+            for (int s = 0; s < a.split; ++s, p += part) {
+                const f32x4_t lo = *(const f32x4_t *)p, hi = *(const f32x4_t *)(p + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += lo[j], v[4 + j] += hi[j];
+                if (OP == kFfnUp) {
+                    const float *q = p + rows * a.N;
+                    const f32x4_t lo = *(const f32x4_t *)q, hi = *(const f32x4_t *)(q + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] += lo[j], w[4 + j] += hi[j];
+                }
+            }
+        }
+        auto put = [&](void *to, size_t at, const float *x) {
+#pragma unroll
+            for (int j = 0; j < 8; j += Piece<ET>::N) *(u32x4_t *)((ET *)to + at + j) = Piece<ET>::pack(x + j);
+        };
+        auto get = [&](const void *from, size_t at, float *x) {
+#pragma unroll
+            for (int j = 0; j < 8; j += Piece<ET>::N) Piece<ET>::unpack(*(const u32x4_t *)((const ET *)from + at + j), x + j);
+        };
+        const size_t at = row * a.N + n;
+        if (OP == kFfnUp) {
+            if (a.o0) put(a.o0, row * a.ldo + n, v), put(a.o1, row * a.ldo + n, w);
+            if (a.o2) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = v[j] * sigmoid<ET>(v[j]) * w[j];
+                put(a.o2, at, v);
+            }
+        } else if (OP == kFfnDh) {
+            if (a.o2) put(a.o2, at, v);
+            if (a.o0) {
+                float g[8], u[8];
+                get(a.g, row * a.ldg + n, g);
+                get(a.u, row * a.ldg + n, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float s = sigmoid<ET>(g[j]);
+                    w[j] = used ? v[j] * (g[j] * s) : 0.f;
+                    v[j] = used ? v[j] * (u[j] * (s * (1.f + g[j] * (1.f - s)))) : 0.f;
+                }
+                put(a.o0, row * a.ldo + n, v);
+                put(a.o1, row * a.ldo + n, w);
+            }
+        } else if (DW) {
+            const size_t e = row / a.M;
+            put(matrix ? a.o1 : a.o0, e * a.eo + (row - e * a.M) * a.ldo + n, v);
+        } else {
+            put(a.o0, at, v);
+        }
     }
 }
 

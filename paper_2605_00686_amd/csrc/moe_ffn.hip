@@ -1,6 +1,8 @@
 // C ABI of the experts' products as calls of their own: argument checks and launches.  Declarations and contracts live in include/moe.h.
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 #include "ffn.hpp"
 #include "problem.hpp"
 
@@ -26,20 +28,79 @@ static int compute_units(int *n) {
     return MOE_OK;
 }
 
-// How a product is launched: workgroups, and whether their tiles are planned.
+// How a product is launched: workgroups, whether their tiles are planned, and what joins the parts of a reduction that is cut.
 struct Launch {
-    const void *kernel;
+    const void *kernel, *join;
     unsigned groups, smem;
     int bm;
     bool planned;
 };
-// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own.
+// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us).  (Tiles of 32 rows take the same each.)
 constexpr int kPlannedTiles = 2;
+
+// The tiles there are to choose from, and what they take where all CUs have them: us for 64 bytes of the reduction, at the start and end, and
+// (256 rows) for 64 rows that a block lacks.  Measured, 16384 rows x 2048 x 2048 on 8 experts, 1.55 to 1.75 GHz: bf16 256 x 256 0.80 us a stage with
+// 256 rows, 0.38 with 64; 128 x 128, two of them per CU, 0.55; 32 x 256 0.26 and 32 x 128 0.14 (more where the weights come from memory:
+// 128 tokens x 8 of 128 of 2048 x 768 0.47); fp32 128 x 128 1.58, 64 x 128 1.02.
+struct Kind {
+    int bm, bn, occ;
+    double stage_us, more_us, less_us;
+};
+constexpr int kKinds = 4;
+constexpr Kind kKindsBf16[kKinds] = {{256, 256, 1, 0.82, 12, 0.14}, {128, 128, 2, 0.56, 7, 0}, {32, 256, 1, 0.35, 6, 0}, {32, 128, 1, 0.18, 5, 0}};
+constexpr Kind kKindsF32[2] = {{128, 128, 2, 1.6, 7, 0}, {64, 128, 2, 1.02, 5, 0}};
+template <typename ET, int KIND> struct TileOf;
+template <> struct TileOf<bf16_t, 0> { typedef FfnTile<bf16_t, 4, 4, 2, 2, 1, 64, 1> type; };
+template <> struct TileOf<bf16_t, 1> { typedef FfnTile<bf16_t, 2, 2, 2, 2, 1, 64, 2> type; };
+template <> struct TileOf<bf16_t, 2> { typedef FfnTile<bf16_t, 1, 2, 1, 4, 1, 128, 1> type; };
+template <> struct TileOf<bf16_t, 3> { typedef FfnTile<bf16_t, 1, 2, 1, 2, 2, 128, 1> type; };
+template <> struct TileOf<float, 0> { typedef FfnTile<float, 2, 2, 2, 2, 1, 64, 2> type; };
+template <> struct TileOf<float, 1> { typedef FfnTile<float, 1, 2, 2, 2, 1, 64, 2> type; };
+
+// The tile, and the parts of the reduction, that take least by what they are worth.  (256 CUs, whatever the card: the workspace goes by it.)
+constexpr int kCus = 256, kMostParts = 32;
+constexpr size_t kPartBytes = (size_t)32 << 20;  // of parts' sums, at most
+struct Choice {
+    int kind, split;
+    size_t part_bytes;
+};
+static Choice choose(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {
+    const int slots = p->T * p->k, experts = p->E < slots ? p->E : slots, sz = elem_bytes(p);
+    const int mats = op == kFfnUp || (op == kFfnDw && !a.down) ? 2 : 1;  // (dW1 and dW3: alone as together, for the same bits)
+    const double rows = (double)slots / experts;  // of an expert that has any, about
+    Choice best = {0, 1, 0};
+    double best_us = 0;
+    for (int k = 0; k < (sz == 4 || op == kFfnDw ? 2 : kKinds); ++k) {
+#ifdef FORCE_KIND
+        if (k != FORCE_KIND) continue;
+#endif
+        const Kind &t = sz == 2 ? kKindsBf16[k] : kKindsF32[k];
+        const int cols = op == kFfnUp ? t.bn / 2 : t.bn;
+        const double nt = (double)((a.N + cols - 1) / cols) * (op == kFfnDw ? mats : 1);
+        // row blocks, half a one more per expert than its rows fill, and how many times 64 rows one lacks
+        const double per_expert = rows / t.bm + 0.5 > 1 ? rows / t.bm + 0.5 : 1;
+        const double blocks = op == kFfnDw ? (double)p->E * ((a.M + t.bm - 1) / t.bm) : experts * per_expert;
+        const double lacks = op == kFfnDw ? 0 : floor((t.bm - rows / per_expert) / 64);
+        const double stages = op == kFfnDw ? rows * sz / 64 : (op == kFfnDx ? 2.0 : 1.0) * a.K * sz / 64;
+        for (int s = 1; s <= kMostParts; s *= 2) {
+#ifdef FORCE_SPLIT
+            if (s != FORCE_SPLIT) continue;
+#endif
+            if (s > 1 && stages / s < 8) break;
+            const size_t bytes = s == 1 ? 0 : (size_t)s * (op == kFfnDw ? (size_t)p->E * a.M : (size_t)a.rows) * a.N * mats * 4;
+            if (bytes > kPartBytes) break;
+            const double per = blocks * nt * s / (kCus * t.occ), rounds = per <= 1 ? 1 : per + 0.5;
+            const double us = rounds * (stages / s * (t.stage_us - lacks * t.less_us) + t.more_us) + (s > 1 ? 6 + bytes / 2e6 : 0);
+            if (best_us == 0 || us < best_us) best_us = us, best = {k, s, bytes};
+        }
+    }
+    return best;
+}
 
 template <class T, FfnOp OP>
 static int prepare(FfnArgs &a, Launch *l) {
     constexpr int COLS = OP == kFfnUp ? T::BN / 2 : T::BN;
-    a.nt = (a.N + COLS - 1) / COLS * (OP == kFfnDw && a.o1 ? 2 : 1);
+    a.nt = (a.N + COLS - 1) / COLS * (OP == kFfnDw && a.o1 ? 2 : 1) * a.split;
     a.mt = (a.M + T::BM - 1) / T::BM;
     // row blocks, at most: one per BM rows and one more per expert (ragged: and for the rows behind the last one)
     size_t blocks;
@@ -55,59 +116,45 @@ static int prepare(FfnArgs &a, Launch *l) {
     if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
     const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * T::OCC;
     l->kernel = (const void *)k_ffn<T, OP>;
+    l->join = a.split > 1 ? (const void *)k_ffn_join<typename T::ET, OP> : nullptr;
     l->groups = (unsigned)(tiles < room ? tiles : room);
     l->smem = T::SMEM;
     l->bm = T::BM;
-    l->planned = tiles >= kPlannedTiles * room;
+    l->planned = T::BM >= 64 && tiles >= kPlannedTiles * room;
     return MOE_OK;
 }
-
 template <typename ET, FfnOp OP>
-static int pick(FfnArgs &a, int slots, Launch *l) {
-    if constexpr (sizeof(ET) == 4) {
-        return slots / a.E > 48 ? prepare<FfnTile<ET, 2, 2, 2, 2, 64, 2>, OP>(a, l) : prepare<FfnTile<ET, 1, 2, 1, 4, 64, 2>, OP>(a, l);
-    } else {
-#ifndef V256
-#define V256 4, 4, 2, 2, 64, 1
-#endif
-#ifndef V128
-#define V128 4, 4, 2, 2, 64, 1
-#endif
-#ifndef V32
-#define V32 1, 2, 1, 4, 128, 1
-#endif
-        if (slots / a.E > 160) return prepare<FfnTile<ET, V256>, OP>(a, l);
-        return slots / a.E > 48 ? prepare<FfnTile<ET, V128>, OP>(a, l) : prepare<FfnTile<ET, V32>, OP>(a, l);
+static int prepare(int kind, FfnArgs &a, Launch *l) {
+    if (kind == 0) return prepare<typename TileOf<ET, 0>::type, OP>(a, l);
+    if (kind == 1) return prepare<typename TileOf<ET, 1>::type, OP>(a, l);
+    if constexpr (OP != kFfnDw && sizeof(ET) == 2) {
+        if (kind == 2) return prepare<typename TileOf<ET, 2>::type, OP>(a, l);
+        return prepare<typename TileOf<ET, 3>::type, OP>(a, l);
     }
-}
-template <typename ET>
-static int pick_dw(FfnArgs &a, Launch *l) {
-    if constexpr (sizeof(ET) == 4)
-        return prepare<FfnTile<ET, 2, 2, 2, 2, 64, 2>, kFfnDw>(a, l);
-    else
-#ifndef VDW
-#define VDW 4, 4, 2, 2, 64, 1
-#endif
-        return prepare<FfnTile<ET, VDW>, kFfnDw>(a, l);
+    return MOE_ERR_UNSUPPORTED;  // (no such kind)
 }
 template <FfnOp OP>
-static int pick(const moe_problem_t *p, FfnArgs &a, Launch *l) {
-    if constexpr (OP == kFfnDw)
-        return p->dtype == MOE_DT_F32 ? pick_dw<float>(a, l) : pick_dw<bf16_t>(a, l);
-    else
-        return p->dtype == MOE_DT_F32 ? pick<float, OP>(a, p->T * p->k, l) : pick<bf16_t, OP>(a, p->T * p->k, l);
+static int prepare(const moe_problem_t *p, FfnArgs &a, float *part, Launch *l) {
+    const Choice c = choose(p, OP, a);
+    a.split = c.split, a.part = part;
+    return p->dtype == MOE_DT_F32 ? prepare<float, OP>(c.kind, a, l) : prepare<bf16_t, OP>(c.kind, a, l);
 }
+// The workspace: two plans, then the parts' sums of one product.
+static FfnPlan *plans_of(void *workspace) { return (FfnPlan *)workspace; }
+static float *parts_of(void *workspace) { return (float *)((char *)workspace + (2 * sizeof(FfnPlan) + 255) / 256 * 256); }
+
 // A call's launches: a product of rows (any but dw), dw, or both.
 template <FfnOp OP>
 static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *workspace, void *stream) {
     hipStream_t st = (hipStream_t)stream;
     Launch l[2] = {};
     FfnArgs *a[2] = {rows, dw};
+    float *parts = parts_of(workspace);
     if (rows)
-        if (const int rc = pick<OP>(p, *rows, &l[0])) return rc;
+        if (const int rc = prepare<OP>(p, *rows, parts, &l[0])) return rc;
     if (dw)
-        if (const int rc = pick<kFfnDw>(p, *dw, &l[1])) return rc;
-    FfnPlan *plans = (FfnPlan *)workspace;
+        if (const int rc = prepare<kFfnDw>(p, *dw, parts, &l[1])) return rc;
+    FfnPlan *plans = plans_of(workspace);
     if (l[0].planned || l[1].planned) {
         FfnPlanArgs plan = {};
         if (l[0].planned) plan.rows = *rows, plan.rows_plan = plans, plan.bm = l[0].bm, rows->plan = plans;
@@ -119,18 +166,34 @@ static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *work
         if (!a[i]) continue;
         void *args[] = {a[i]};
         if (hipLaunchKernel(l[i].kernel, dim3(l[i].groups), dim3(kThreads), args, l[i].smem, st) != hipSuccess) return MOE_ERR_HIP;
+        if (!l[i].join) continue;
+        const size_t pieces = (i ? (size_t)a[i]->E * a[i]->M * (a[i]->o1 ? 2 : 1) : (size_t)a[i]->rows) * (a[i]->N / 8), groups = (pieces + kThreads - 1) / kThreads;
+        if (hipLaunchKernel(l[i].join, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(kThreads), args, 0, st) != hipSuccess) return MOE_ERR_HIP;
     }
     return MOE_OK;
 }
 static FfnArgs args_of(const moe_problem_t *p, const int32_t *counts) {
     FfnArgs a = {};
-    a.E = p->E; a.rows = rows_of(p); a.capacity = p->capacity; a.counts = counts;
+    a.E = p->E; a.rows = rows_of(p); a.capacity = p->capacity; a.counts = counts; a.split = 1;
     return a;
 }
 
 extern "C" {
 
-size_t moe_ffn_workspace_bytes(const moe_problem_t *p) { return check_problem(p) == MOE_OK ? (2 * sizeof(FfnPlan) + 255) / 256 * 256 : 0; }
+size_t moe_ffn_workspace_bytes(const moe_problem_t *p) {
+    if (check_problem(p) != MOE_OK) return 0;
+    size_t parts = 0;
+    for (int i = 0; i < 6; ++i) {
+        FfnArgs a = args_of(p, nullptr);
+        const FfnOp op = (FfnOp)(i < kFfnDw ? i : kFfnDw);
+        const bool down = i == kFfnDw;  // dW2; 5: dW1 and dW3
+        a.down = down, a.M = down ? p->f : p->d, a.N = op == kFfnDw ? (down ? p->d : p->f) : op == kFfnUp || op == kFfnDh ? p->f : p->d;
+        a.K = op == kFfnUp || op == kFfnDh ? p->d : p->f;
+        const size_t bytes = choose(p, op, a).part_bytes;
+        if (bytes > parts) parts = bytes;
+    }
+    return (size_t)((char *)parts_of(nullptr) - (char *)nullptr) + (parts + 255) / 256 * 256;
+}
 
 static int check_workspace(const void *ws) { return !ws || ((uintptr_t)ws & 255) != 0 ? MOE_ERR_WORKSPACE : MOE_OK; }
 
@@ -186,7 +249,7 @@ int moe_ffn_down_backward(const moe_problem_t *p, const void *dy, const void *W2
     }
     {
         FfnArgs &a = dw;
-        a.M = p->f; a.N = p->d;
+        a.down = true; a.M = p->f; a.N = p->d;
         a.A0 = h; a.lda = p->f;
         a.B0 = dy; a.ldb = p->d;
         a.o0 = dW2; a.ldo = p->d; a.eo = (long long)p->f * p->d;
