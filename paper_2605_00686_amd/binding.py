@@ -216,22 +216,40 @@ def moe_ffn_workspace_bytes(p: MoeProblem) -> int:
 
 def _like_rows(*tensors):
     """[rows, f] tensors or views (or None) whose rows are the same number of elements apart: that number, and their addresses."""
-    given = [t for t in tensors if t is not None]
-    if not given:
-        return (0,) + (None,) * len(tensors)
-    (rows, f), ld = given[0].shape, given[0].stride(0)
-    for t in given:
-        assert t.is_cuda and t.shape == given[0].shape and (f == 1 or t.stride(1) == 1), "device tensors, rows of one piece"
-        assert rows == 1 or t.stride(0) == ld, "rows the same number of elements apart"
-    return (ld if rows > 1 else f,) + tuple(None if t is None else t.data_ptr() for t in tensors)
+    shape = None
+    out = [0]
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if shape is None:
+            shape = t.shape
+            rows, f = shape
+            out[0] = ld = t.stride(0) if rows > 1 else f
+        step = t.stride()
+        assert t.is_cuda and t.shape == shape and (step[1] == 1 or f == 1), "device tensors, rows of one piece"
+        assert rows == 1 or step[0] == ld, "rows the same number of elements apart"
+        out.append(t.data_ptr())
+    return out
 
 
 def _like_matrices(*tensors):
     """[E, d, f] tensors or views (or None), matrix behind matrix, whose rows are the same number of elements apart: as _like_rows."""
+    shape = None
+    out = [0]
     for t in tensors:
-        if t is not None:
-            assert t.dim() == 3 and (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1)), "matrix behind matrix"
-    return _like_rows(*(None if t is None else t.flatten(0, 1) for t in tensors))
+        if t is None:
+            out.append(None)
+            continue
+        if shape is None:
+            shape = t.shape
+            E, d, f = shape
+            out[0] = ld = t.stride(1) if d > 1 else t.stride(0) if E > 1 else f
+        step = t.stride()
+        assert t.is_cuda and t.shape == shape and (step[2] == 1 or f == 1), "device tensors, rows of one piece"
+        assert (d == 1 or step[1] == ld) and (E == 1 or step[0] == d * ld), "rows the same number of elements apart, matrix behind matrix"
+        out.append(t.data_ptr())
+    return out
 
 
 def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):

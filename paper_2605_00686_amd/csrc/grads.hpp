@@ -6,15 +6,13 @@
 // number is read for the norm, and read and written for the scaling; the conversions and fused products in 64 bits are a third of what the
 // vector ALU could do meanwhile.  Tensors are cut into chunks that the workgroups go through in turn, sums are added in a fixed order.
 #pragma once
-#include <type_traits>
-
 #include "pieces.hpp"
 
 namespace moe {
 
-constexpr int kGradTensors = 96;     // per launch: their places are kernel arguments
+constexpr int kGradTensors = 140;    // per launch: their places are kernel arguments
 constexpr int kGradPieces = 8;       // of 16 bytes per thread and chunk
-constexpr int kGradGroups = 2048;    // workgroups, at most
+constexpr int kGradGroups = 4096;    // workgroups, at most
 
 struct GradArgs {
     int n, f32[(kGradTensors + 31) / 32];  // tensors; a bit each: fp32 (else bf16)
@@ -28,41 +26,63 @@ struct GradArgs {
 };
 static_assert(sizeof(GradArgs) <= 4096, "kernel arguments");
 
-// Eight or four numbers of a tensor that starts anywhere.
+// 16 bytes of a tensor that starts anywhere.
 struct __attribute__((packed)) Unaligned16 {
     u32x4_t v;
 };
 
-// f(piece of 16 bytes, its numbers there are) for the pieces of the thread in the workgroup's chunks
-template <class Whole, class Rest>
-__device__ __forceinline__ void for_each_chunk(const GradArgs &a, Whole whole, Rest rest) {
+// f(tensor, whether it is fp32, its first number, how many) for the workgroup's chunks
+template <class F>
+__device__ __forceinline__ void for_each_chunk(const GradArgs &a, F f) {
     constexpr u32 kChunk = kThreads * kGradPieces;  // pieces
-    const u32 chunks = a.n ? a.end[a.n - 1] : 0;
-    int t = 0;
+    const u32 chunks = a.end[a.n - 1];
+    int t = -1;
     for (u32 c = blockIdx.x; c < chunks; c += gridDim.x) {
+        if (t < 0) {  // the first tensor that ends behind the chunk
+            int lo = 0, hi = a.n - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (c < a.end[mid])
+                    hi = mid;
+                else
+                    lo = mid + 1;
+            }
+            t = lo;
+        }
         while (c >= a.end[t]) ++t;
         const u32 in = c - (t ? a.end[t - 1] : 0);
         const bool f32 = a.f32[t >> 5] >> (t & 31) & 1;
-        const int per = f32 ? 4 : 8;
-        const long long first = (long long)in * kChunk * per, left = a.count[t] - first;
-        if (left >= (long long)kChunk * per)
-            whole(t, f32, first);
-        else
-            rest(t, f32, first, (int)left);
+        const long long each = (long long)kChunk * (f32 ? 4 : 8), first = in * each;
+        f(t, f32, first, (int)min(a.count[t] - first, each));
     }
 }
-
-template <bool F32>
-__device__ __forceinline__ double square_sum(const u32x4_t &v, double s) {
-    typedef Piece<typename std::conditional<F32, float, bf16_t>::type> P;
-    float f[P::N];
-    P::unpack(v, f);
+// The thread's pieces of a chunk of `n` numbers: whole ones in v, zeros where there is none; returns how many numbers the one piece that the
+// tensor ends inside has, if it is the thread's (its number in *part).
+template <int PER>
+__device__ __forceinline__ int load_pieces(const void *p, int n, u32x4_t (&v)[kGradPieces], int *part) {
+    int rest = 0;
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) s = fma((double)f[i], (double)f[i], s);
+    for (int i = 0; i < kGradPieces; ++i) {
+        const int k = (int)threadIdx.x + i * kThreads;
+        v[i] = u32x4_t{0, 0, 0, 0};
+        if ((k + 1) * PER <= n)
+            v[i] = ((const Unaligned16 *)p)[k].v;
+        else if (k * PER < n)
+            rest = n - k * PER, *part = k;
+    }
+    return rest;
+}
+
+template <typename ET>
+__device__ __forceinline__ double square_sum(const u32x4_t &v, double s) {
+    float f[Piece<ET>::N];
+    Piece<ET>::unpack(v, f);
+#pragma unroll
+    for (int i = 0; i < Piece<ET>::N; ++i) s = fma((double)f[i], (double)f[i], s);
     return s;
 }
-__device__ __forceinline__ float grad_at(const void *p, bool f32, long long i) { return f32 ? ((const float *)p)[i] : bf16_to_f32(((const bf16_t *)p)[i]); }
 
+template <int THREADS>
 __device__ __forceinline__ double sum_workgroup(double v, double *lds) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
@@ -70,38 +90,43 @@ __device__ __forceinline__ double sum_workgroup(double v, double *lds) {
     __syncthreads();
     v = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) v += lds[w];
+    for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
     return v;
 }
 
 __global__ __launch_bounds__(kThreads) void k_grad_squares(GradArgs a) {
     __shared__ double lds[kThreads / 64];
     double s = 0;
-    for_each_chunk(
-        a,
-        [&](int t, bool f32, long long first) {
-            const Unaligned16 *p = (const Unaligned16 *)((const char *)a.in[t] + first * (f32 ? 4 : 2)) + threadIdx.x;
+    for_each_chunk(a, [&](int t, bool f32, long long first, int n) {
+        auto chunk = [&](auto zero) {
+            typedef decltype(zero) ET;
+            constexpr int PER = Piece<ET>::N;
+            const ET *p = (const ET *)a.in[t] + first;
             u32x4_t v[kGradPieces];
+            int part = 0;
+            const int rest = load_pieces<PER>(p, n, v, &part);
 #pragma unroll
-            for (int i = 0; i < kGradPieces; ++i) v[i] = p[i * kThreads].v;
-#pragma unroll
-            for (int i = 0; i < kGradPieces; ++i) s = f32 ? square_sum<true>(v[i], s) : square_sum<false>(v[i], s);
-        },
-        [&](int t, bool f32, long long first, int left) {
-            for (int i = threadIdx.x; i < left; i += kThreads) {
-                const double g = grad_at(a.in[t], f32, first + i);
+            for (int i = 0; i < kGradPieces; ++i) s = square_sum<ET>(v[i], s);
+            for (int i = 0; i < rest; ++i) {
+                const double g = Elem<ET>::load(p, (size_t)part * PER + i);
                 s = fma(g, g, s);
             }
-        });
-    s = sum_workgroup(s, lds);
+        };
+        if (f32)
+            chunk(0.f);
+        else
+            chunk(bf16_t{0});
+    });
+    s = sum_workgroup<kThreads>(s, lds);
     if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_grad_norm(const double *parts, int n, double *sum, float *norm) {
-    __shared__ double lds[kThreads / 64];
+constexpr int kGradNormThreads = 1024;
+__global__ __launch_bounds__(kGradNormThreads) void k_grad_norm(const double *parts, int n, double *sum, float *norm) {
+    __shared__ double lds[kGradNormThreads / 64];
     double s = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) s += parts[i];
-    s = sum_workgroup(s, lds);
+    for (int i = threadIdx.x; i < n; i += kGradNormThreads) s += parts[i];
+    s = sum_workgroup<kGradNormThreads>(s, lds);
     if (threadIdx.x) return;
     *sum = s;
     if (norm) *norm = (float)sqrt(s);
@@ -113,40 +138,50 @@ __device__ __forceinline__ double clip_factor(double sum, float max_norm) {
     return norm > max_norm && norm < __builtin_inf() ? max_norm / norm : 1.0;
 }
 // fp32 in 64 bits and bf16 in 32: one rounding that counts
-template <bool F32>
-__device__ __forceinline__ u32x4_t scaled(const u32x4_t &v, double factor) {
-    typedef Piece<typename std::conditional<F32, float, bf16_t>::type> P;
-    float f[P::N];
-    P::unpack(v, f);
-#pragma unroll
-    for (int i = 0; i < P::N; ++i) f[i] = F32 ? (float)(f[i] * factor) : f[i] * (float)factor;
-    return P::pack(f);
-}
+__device__ __forceinline__ float scaled(float g, double factor, float) { return (float)(g * factor); }
+__device__ __forceinline__ float scaled(float g, double factor, bf16_t) { return g * (float)factor; }
 
 __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
     const double factor = clip_factor(*a.sum, a.max_norm);
-    for_each_chunk(
-        a,
-        [&](int t, bool f32, long long first) {
-            if (factor == 1.0 && a.in[t] == a.out[t]) return;
-            const Unaligned16 *p = (const Unaligned16 *)((const char *)a.in[t] + first * (f32 ? 4 : 2)) + threadIdx.x;
-            Unaligned16 *q = (Unaligned16 *)((char *)a.out[t] + first * (f32 ? 4 : 2)) + threadIdx.x;
+    for_each_chunk(a, [&](int t, bool f32, long long first, int n) {
+        if (factor == 1.0 && a.in[t] == a.out[t]) return;
+        auto chunk = [&](auto zero) {
+            typedef decltype(zero) ET;
+            constexpr int PER = Piece<ET>::N;
+            const ET *p = (const ET *)a.in[t] + first;
+            ET *q = (ET *)a.out[t] + first;
             u32x4_t v[kGradPieces];
+            int part = 0;
+            const int rest = load_pieces<PER>(p, n, v, &part);
+            const bool aligned = ((uintptr_t)q & 15) == 0;
 #pragma unroll
-            for (int i = 0; i < kGradPieces; ++i) v[i] = p[i * kThreads].v;
+            for (int i = 0; i < kGradPieces; ++i) {
+                const int k = (int)threadIdx.x + i * kThreads;
+                if ((k + 1) * PER > n) continue;
+                float f[PER];
+                Piece<ET>::unpack(v[i], f);
 #pragma unroll
-            for (int i = 0; i < kGradPieces; ++i) q[i * kThreads].v = f32 ? scaled<true>(v[i], factor) : scaled<false>(v[i], factor);
-        },
-        [&](int t, bool f32, long long first, int left) {
-            if (factor == 1.0 && a.in[t] == a.out[t]) return;
-            for (int i = threadIdx.x; i < left; i += kThreads) {
-                const float g = grad_at(a.in[t], f32, first + i);
-                if (f32)
-                    ((float *)a.out[t])[first + i] = (float)(g * factor);
+                for (int j = 0; j < PER; ++j) f[j] = scaled(f[j], factor, zero);
+                const u32x4_t w = Piece<ET>::pack(f);
+                if (aligned)
+                    store_past((u32x4_t *)q + k, w);
                 else
-                    ((bf16_t *)a.out[t])[first + i] = (bf16_t)pack_bf16x2(g * (float)factor, 0.f);
+                    ((Unaligned16 *)q)[k].v = w;
             }
-        });
+            for (int i = 0; i < rest; ++i) {
+                const size_t at = (size_t)part * PER + i;
+                const float g = scaled(Elem<ET>::load(p, at), factor, zero);
+                if constexpr (sizeof(ET) == 4)
+                    q[at] = g;
+                else
+                    q[at] = (bf16_t)pack_bf16x2(g, 0.f);
+            }
+        };
+        if (f32)
+            chunk(0.f);
+        else
+            chunk(bf16_t{0});
+    });
 }
 
 }  // namespace moe

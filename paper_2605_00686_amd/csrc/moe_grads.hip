@@ -68,7 +68,7 @@ int moe_grad_norm(const moe_tensor_t *tensors, int32_t n, double *sum_squares, f
         if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
         done += (int)groups;
     }
-    hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(kThreads), 0, st, (const double *)parts, done, sum_squares, norm);
+    hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(kGradNormThreads), 0, st, (const double *)parts, done, sum_squares, norm);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

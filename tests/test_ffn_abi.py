@@ -76,8 +76,8 @@ class Rows:  # a device tensor as far as the binding looks
     def dim(self):
         return len(self.shape)
 
-    def stride(self, i):
-        return self._s[i]
+    def stride(self, i=None):
+        return self._s if i is None else self._s[i]
 
     def data_ptr(self):
         return 0x10000
@@ -85,15 +85,16 @@ class Rows:  # a device tensor as far as the binding looks
 
 def test_views_that_are_not_alike_are_refused():
     ok = Rows((4, 64), (128, 1))
-    assert B._like_rows(ok, None, ok) == (128, 0x10000, None, 0x10000)
-    assert B._like_rows(None, None) == (0, None, None)
+    assert B._like_rows(ok, None, ok) == [128, 0x10000, None, 0x10000]
+    assert B._like_rows(None, None) == [0, None, None]
     for bad in (Rows((4, 64), (64, 1)), Rows((4, 64), (128, 4)), Rows((4, 32), (128, 1))):
         with pytest.raises(AssertionError):
             B._like_rows(ok, bad)
-    with pytest.raises(AssertionError):
-        B._like_matrices(Rows((3, 4, 64), (512, 64, 1)))
-    with pytest.raises(AssertionError):
-        B._like_matrices(Rows((4, 64), (64, 1)))
+    whole, half = Rows((3, 4, 64), (256, 64, 1)), Rows((3, 4, 64), (512, 128, 1))
+    assert B._like_matrices(whole, None) == [64, 0x10000, None] and B._like_matrices(None, half) == [128, None, 0x10000]
+    for bad in (Rows((3, 4, 64), (512, 64, 1)), Rows((3, 4, 64), (256, 64, 2)), half):
+        with pytest.raises(AssertionError):
+            B._like_matrices(whole, bad)
 
 
 def tensors(*given):
