@@ -31,25 +31,21 @@ struct __attribute__((packed)) Unaligned16 {
     u32x4_t v;
 };
 
-// f(tensor, whether it is fp32, its first number, how many) for the workgroup's chunks
-template <class F>
+// f(tensor, whether it is fp32, its first number, how many) for the workgroup's chunks, from the last one on if BACK
+template <bool BACK, class F>
 __device__ __forceinline__ void for_each_chunk(const GradArgs &a, F f) {
     constexpr u32 kChunk = kThreads * kGradPieces;  // pieces
     const u32 chunks = a.end[a.n - 1];
-    int t = -1;
-    for (u32 c = blockIdx.x; c < chunks; c += gridDim.x) {
-        if (t < 0) {  // the first tensor that ends behind the chunk
-            int lo = 0, hi = a.n - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (c < a.end[mid])
-                    hi = mid;
-                else
-                    lo = mid + 1;
-            }
-            t = lo;
+    for (u32 i = blockIdx.x; i < chunks; i += gridDim.x) {
+        const u32 c = BACK ? chunks - 1 - i : i;
+        int t = 0, hi = a.n - 1;  // the first tensor that ends behind the chunk
+        while (t < hi) {
+            const int mid = (t + hi) / 2;
+            if (c < a.end[mid])
+                hi = mid;
+            else
+                t = mid + 1;
         }
-        while (c >= a.end[t]) ++t;
         const u32 in = c - (t ? a.end[t - 1] : 0);
         const bool f32 = a.f32[t >> 5] >> (t & 31) & 1;
         const long long each = (long long)kChunk * (f32 ? 4 : 8), first = in * each;
@@ -97,7 +93,7 @@ __device__ __forceinline__ double sum_workgroup(double v, double *lds) {
 __global__ __launch_bounds__(kThreads) void k_grad_squares(GradArgs a) {
     __shared__ double lds[kThreads / 64];
     double s = 0;
-    for_each_chunk(a, [&](int t, bool f32, long long first, int n) {
+    for_each_chunk<false>(a, [&](int t, bool f32, long long first, int n) {
         auto chunk = [&](auto zero) {
             typedef decltype(zero) ET;
             constexpr int PER = Piece<ET>::N;
@@ -143,7 +139,8 @@ __device__ __forceinline__ float scaled(float g, double factor, bf16_t) { return
 
 __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
     const double factor = clip_factor(*a.sum, a.max_norm);
-    for_each_chunk(a, [&](int t, bool f32, long long first, int n) {
+    // (backwards: the norm has left the last numbers in the caches)
+    for_each_chunk<true>(a, [&](int t, bool f32, long long first, int n) {
         if (factor == 1.0 && a.in[t] == a.out[t]) return;
         auto chunk = [&](auto zero) {
             typedef decltype(zero) ET;
