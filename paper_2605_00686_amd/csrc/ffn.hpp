@@ -78,6 +78,7 @@ struct Segment {
 struct FfnTables {
     int begin[kMaxExperts + 1], used[kMaxExperts];  // begin[E]: behind the last one's (ragged)
     int first[kMaxExperts + 1];  // first row block of an expert, of the rows of nobody behind the last (ragged); dw: rows before, and kDwStart for each expert
+    int order[kMaxExperts];      // dw's plan: the tiles are in this order of experts
     int edge[kTileQueues + 1];   // tiles [edge[x], edge[x + 1]) are XCD x's
     int next;                    // in a workgroup's copy: the tile it takes next
     u64 sum[8];                  // scratch
@@ -97,6 +98,10 @@ struct FfnTile {
     static constexpr int ROOM = (160 * 1024 / OCC - (int)sizeof(FfnTables)) / 1024 * 1024, SMEM = ROOM + (int)sizeof(FfnTables);
     static constexpr int stage_bytes(int live) { return (BN + BM / MB * live) * KB; }  // of a tile with `live` row blocks per wavefront
     static constexpr int stages(int live) { return ROOM / stage_bytes(live) < 7 ? ROOM / stage_bytes(live) : 7; }
+    // fp32: sums of this many stages are added up apart, where there are registers for them (64 rows; 128 rows would spill 100 of them and more).
+    // A sum's roundings, six per 16 steps, are those of its length.  512 x 2 of 8 experts of 8192 x 2048, dx, 2-norm of the error against 64 bits:
+    // one sum of 16384 steps 1.1e-6, sums of 32 stages 4e-7.
+    static constexpr int SUM_STAGES = sizeof(ET) == 4 && MB * NB <= 2 ? 32 : 0;
     static_assert(WAVES * 64 == kThreads, "threads");
 };
 
@@ -187,6 +192,33 @@ __device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables 
     }
 }
 
+// dw: a plan deals the experts out to the XCDs by their rows, from the largest to the smallest and back again, and each XCD begins with its largest.
+// (For fewer experts, stretches of the same work are more even.)  us, in the experts' order / by rows: 4096 x 8 of 128 of 2048 x 768 dW2 233 / 219,
+// dW1 and dW3 418 / 404.  The products of rows stay in the experts' order: their short tiles, which wait for weights, side by side at the end
+// take longer than mixed with the others, up 329 / 351, dx 341 / 361.
+constexpr int kDealtExperts = 32;
+__device__ __forceinline__ void deal_experts(const FfnArgs &a, FfnTables *t) {
+    const int tid = threadIdx.x, mine = tid < a.E ? t->used[tid] : 0;
+    if (a.E < kDealtExperts) {
+        if (tid < a.E) t->order[tid] = tid;
+        __syncthreads();
+        return;
+    }
+    int rank = 0;
+    for (int e = 0; e < a.E; ++e) rank += t->used[e] > mine || (t->used[e] == mine && e < tid);
+    // rank r is number r / 8 of its XCD
+    const int rounds = a.E / kTileQueues, rest = a.E % kTileQueues;
+    auto before = [&](int x) {  // experts of the XCDs before x
+        return x * rounds + (rounds & 1 ? max(x - (kTileQueues - rest), 0) : min(x, rest));
+    };
+    if (tid < a.E) {
+        const int round = rank / kTileQueues, x = round & 1 ? kTileQueues - 1 - rank % kTileQueues : rank % kTileQueues;
+        t->order[before(x) + round] = tid;
+    }
+    if (tid <= kTileQueues) t->edge[tid] = before(tid) * a.mt * a.nt;
+    __syncthreads();
+}
+
 // One workgroup makes the tables for the launch or two that follow.
 struct FfnPlanArgs {
     FfnArgs rows, dw;  // the launches'
@@ -202,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void k_ffn_plan(FfnPlanArgs a) {
         __syncthreads();
     };
     if (a.rows_plan) make_tables<false>(a.rows, a.bm, &t), out(a.rows_plan);
-    if (a.dw_plan) make_tables<true>(a.dw, 1, &t), out(a.dw_plan);
+    if (a.dw_plan) make_tables<true>(a.dw, 1, &t), deal_experts(a.dw, &t), out(a.dw_plan);
 }
 
 // The fragments of N blocks of an operand for step `kk` (32 bytes of the reduction) of a stage: lane l has index l & 31 of a block and the
@@ -334,8 +366,9 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         int r, c;
         if (DW) {
             const int per = a.mt * a.nt;
-            w.s.e = t / per, w.s.block = 0;
-            tile_in_groups(t - w.s.e * per, a.mt, a.nt, &r, &c);
+            const int at = t / per;
+            w.s.e = a.plan ? uniform(tables->order[at]) : at, w.s.block = 0;
+            tile_in_groups(t - at * per, a.mt, a.nt, &r, &c);
             w.s.begin = uniform(tables->begin[w.s.e]), w.s.used = w.s.extent = uniform(tables->used[w.s.e]);
             w.row0 = r * T::BM;
             w.end = (w.s.used + STEPS - 1) / STEPS;
@@ -553,16 +586,47 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
 #pragma unroll
                         for (int nb = 0; nb < T::NB; ++nb) multiply<bf16_t>(cb[nb].part[kTerms[t][1]], ca[mb].part[kTerms[t][0]], acc[mb][nb]);
             };
-            read_cut();
-            for (int kt = 1; kt < nk; ++kt) {
-                multiply_cut();
+            auto go_on = [&](int kt) __attribute__((always_inline)) {
                 landed(kt, min(nk - 1 - kt, NS - 2));
                 on();
                 if (next < k0 + nk) load_stage();
                 read_cut();
+            };
+            read_cut();
+            if constexpr (T::SUM_STAGES != 0) {
+                f32x16_t sum[LIVE][T::NB];
+                for (int kt = 1, from = 0;; from = kt - 1) {
+                    const int to = min(nk, from + T::SUM_STAGES);
+                    for (; kt < to; ++kt) {
+                        multiply_cut();
+                        go_on(kt);
+                    }
+                    if (ASK && kt == nk) ask();
+                    multiply_cut();
+                    const bool last = kt == nk;
+                    if (last && from == 0) break;
+#pragma unroll
+                    for (int mb = 0; mb < LIVE; ++mb)
+#pragma unroll
+                        for (int nb = 0; nb < T::NB; ++nb)
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) {
+                                const float x = from ? sum[mb][nb][v] + acc[mb][nb][v] : acc[mb][nb][v];
+                                sum[mb][nb][v] = x;
+                                acc[mb][nb][v] = last ? x : 0.f;
+                            }
+                    if (last) break;
+                    go_on(kt);
+                    ++kt;
+                }
+            } else {
+                for (int kt = 1; kt < nk; ++kt) {
+                    multiply_cut();
+                    go_on(kt);
+                }
+                if (ASK) ask();
+                multiply_cut();
             }
-            if (ASK) ask();
-            multiply_cut();
         } else {
             read(stage, 0, f0);
             first_steps(std::false_type{});
