@@ -288,7 +288,8 @@ __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32
 
 // Eight fp32 numbers as three bf16 numbers each, x = p0 + p1 + p2 with |p1| <= 2^-9 |x| and |p2| <= 2^-18 |x|, off by 2^-27 |x| at most.  Of
 // the nine products of two numbers the six largest are taken; the others come to 2^-26 of the whole.  On the matrix cores those six take 192 cycles
-// for 32 x 32 x 16, the fp32 instructions 512.  A number that is not finite, or that bf16 rounds to one, makes a NaN of every sum that it is in.
+// for 32 x 32 x 16, the fp32 instructions 512.  A number that is not finite, or that bf16 rounds to one, makes a NaN of every sum that it is in; a
+// product that only the rounded numbers' is out of range makes it infinite.
 struct Cut {
     u32x4_t part[3];
 };
@@ -851,14 +852,14 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
             } else {
                 run(std::integral_constant<int, T::MB>{});
             }
-            if constexpr (SZ == 4) {  // with numbers that are not finite again, on the fp32 instructions
+            if constexpr (SZ == 4) {  // again on the fp32 instructions where a sum is not finite: bf16 may have rounded numbers, or their product, out of range
                 bool bad = false;
 #pragma unroll
                 for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
                     for (int nb = 0; nb < T::NB; ++nb)
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) bad |= acc[mb][nb][v] != acc[mb][nb][v];
+                        for (int v = 0; v < 16; ++v) bad |= !(fabsf(acc[mb][nb][v]) <= 3.402823466e38f);
                 if (__syncthreads_or(bad)) {
                     clear();
                     start(now);

@@ -255,6 +255,7 @@ def test_offsets_past_32_bits():
     n[0], n[E - 1] = 20, 30
     W2, h, dy = normal(E, f, d, std=0.02), normal(50, f), normal(50, d)
     assert W2.numel() > 2 ** 31
+    ws = workspace(p)
     y, dh, dW2 = torch.full((50, d), NAN, dtype=bf, device="cuda"), torch.full((50, f), NAN, dtype=bf, device="cuda"), torch.full_like(W2, NAN)
     B.moe_ffn_down(p, h, W2, n, y, ws)
     B.moe_ffn_down_backward(p, dy, W2, h, None, None, n, dh, None, None, dW2, ws)
