@@ -76,7 +76,8 @@ struct Segment {
 };
 // Where every expert's rows lie, and which tiles each XCD takes.
 struct FfnTables {
-    int begin[kMaxExperts + 1], used[kMaxExperts];  // begin[E]: behind the last one's (ragged)
+    __align__(16) int used[kMaxExperts];
+    int begin[kMaxExperts + 1];  // begin[E]: behind the last one's (ragged)
     int first[kMaxExperts + 1];  // first row block of an expert, of the rows of nobody behind the last (ragged); dw: rows before, and kDwStart for each expert
     int order[kMaxExperts];      // dw's plan: the tiles are in this order of experts
     int edge[kTileQueues + 1];   // tiles [edge[x], edge[x + 1]) are XCD x's
@@ -205,7 +206,12 @@ __device__ __forceinline__ void deal_experts(const FfnArgs &a, FfnTables *t) {
         return;
     }
     int rank = 0;
-    for (int e = 0; e < a.E; ++e) rank += t->used[e] > mine || (t->used[e] == mine && e < tid);
+    for (int e = 0; e < a.E; e += 4) {
+        const int4 n = *(const int4 *)&t->used[e];  // (the last ones may be of no expert)
+        const int four[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rank += e + j < a.E && (four[j] > mine || (four[j] == mine && e + j < tid));
+    }
     // rank r is number r / 8 of its XCD
     const int rounds = a.E / kTileQueues, rest = a.E % kTileQueues;
     auto before = [&](int x) {  // experts of the XCDs before x
@@ -219,7 +225,7 @@ __device__ __forceinline__ void deal_experts(const FfnArgs &a, FfnTables *t) {
     __syncthreads();
 }
 
-// One workgroup makes the tables for the launch or two that follow.
+// The tables of a call's products, a workgroup each.
 struct FfnPlanArgs {
     FfnArgs rows, dw;  // the launches'
     FfnPlan *rows_plan, *dw_plan;  // NULL: there is none
@@ -233,8 +239,11 @@ __global__ __launch_bounds__(kThreads) void k_ffn_plan(FfnPlanArgs a) {
         if (tid < kTileQueues) p->taken[tid].v = 0;
         __syncthreads();
     };
-    if (a.rows_plan) make_tables<false>(a.rows, a.bm, &t), out(a.rows_plan);
-    if (a.dw_plan) make_tables<true>(a.dw, 1, &t), deal_experts(a.dw, &t), out(a.dw_plan);
+    if (blockIdx.x == 0) {
+        if (a.rows_plan) make_tables<false>(a.rows, a.bm, &t), out(a.rows_plan);
+    } else if (a.dw_plan) {
+        make_tables<true>(a.dw, 1, &t), deal_experts(a.dw, &t), out(a.dw_plan);
+    }
 }
 
 // The fragments of N blocks of an operand for step `kk` (32 bytes of the reduction) of a stage: lane l has index l & 31 of a block and the
@@ -308,8 +317,9 @@ __device__ __forceinline__ Cut cut_f32(const u32x4_t &lo, const u32x4_t &hi) {
     return c;
 }
 
+// Workgroup `group` of `groups`.  (Unsigned: divisions of signed numbers here took down of 4096 x 4 of 128 of 2880 x 2880 from 580 to 700 us.)
 template <class T, FfnOp OP>
-__global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
+__device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     typedef typename T::ET ET;
     constexpr bool DW = OP == kFfnDw, AK = !DW, BK = OP == kFfnDh || OP == kFfnDx, GATED = OP == kFfnUp;
     typedef Operand<ET, T::BM, AK, T::KB, T::WAVES> OA;
@@ -330,8 +340,8 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     const int row_blocks = uniform(tables->edge[kTileQueues]) / a.nt;  // (dw: of tiles)
     // The tile after this one.  Where there is a plan, tiles are handed out as workgroups come for them, first of the own XCD's list, then of
     // the others': experts' last row blocks, and dw's experts, differ in what they take.
-    int list = blockIdx.x % kTileQueues;
-    const int mine = blockIdx.x / kTileQueues, per_list = gridDim.x / kTileQueues;
+    int list = group % kTileQueues;
+    const int mine = group / kTileQueues, per_list = groups / kTileQueues;
     int taken = 0;  // thread 0: what it was given of `list`
     auto ask = [&]() __attribute__((always_inline)) {
         if (a.plan && tid == 0) taken = (int)atomicAdd(&a.plan->taken[list].v, 1u);
@@ -888,6 +898,22 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
         write_tile(done);
         if (tile < 0) break;
     }
+}
+
+template <class T, FfnOp OP>
+__global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
+    ffn<T, OP>(a, blockIdx.x, gridDim.x);
+}
+// A backward call's two products in one launch: workgroups of dw take the CUs that the rows' product leaves, at its end or, where it is small, from
+// the start.  us, kernels one after the other / this: fp32 256 x 2 of 8 of 512 x 1024 dh and dW2 36 / 29, 1001 x 6 of 48 dx and dW1, dW3 228 / 197;
+// bf16 4096 x 8 of 128 of 2048 x 768 480 / 425 and 745 / 725, 16384 x 2 of 8 of 4096 x 14336 13900 / 13600.
+template <class T, FfnOp OP, class TDW>
+__global__ __launch_bounds__(kThreads, T::OCC) void k_ffn_both(FfnArgs a, FfnArgs dw, u32 first) {
+    static_assert(T::OCC == TDW::OCC && T::SMEM == TDW::SMEM, "room");
+    if (blockIdx.x < first)
+        ffn<T, OP>(a, blockIdx.x, first);
+    else
+        ffn<TDW, kFfnDw>(dw, blockIdx.x - first, gridDim.x - first);
 }
 
 // The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.

@@ -3,6 +3,8 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 #include "ffn.hpp"
 #include "problem.hpp"
 
@@ -32,7 +34,8 @@ static int compute_units(int *n) {
 struct Launch {
     const void *kernel, *join;
     unsigned groups, smem;
-    int bm;
+    size_t part_bytes;
+    int kind, bm;
     bool planned;
 };
 // Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us).  (Tiles of 32 rows take the same each.)
@@ -133,13 +136,32 @@ static int prepare(int kind, FfnArgs &a, Launch *l) {
     }
     return MOE_ERR_UNSUPPORTED;  // (no such kind)
 }
+// The kernel of both products of a backward call, NULL where their workgroups need different room.
+template <typename ET, FfnOp OP, int KIND, int DW>
+static const void *both_of() {
+    typedef typename TileOf<ET, KIND>::type T;
+    typedef typename TileOf<ET, DW>::type TDW;
+    if constexpr ((OP == kFfnDh || OP == kFfnDx) && T::OCC == TDW::OCC)
+        return (const void *)k_ffn_both<T, OP, TDW>;
+    else
+        return nullptr;
+}
+template <typename ET, FfnOp OP>
+static const void *both_of(int kind, int dw) {
+    if (kind == 0) return dw ? both_of<ET, OP, 0, 1>() : both_of<ET, OP, 0, 0>();
+    if (kind == 1) return dw ? both_of<ET, OP, 1, 1>() : both_of<ET, OP, 1, 0>();
+    if constexpr (sizeof(ET) == 2) {
+        if (!dw) return kind == 2 ? both_of<ET, OP, 2, 0>() : both_of<ET, OP, 3, 0>();
+    }
+    return nullptr;
+}
 template <FfnOp OP>
 static int prepare(const moe_problem_t *p, FfnArgs &a, float *part, Launch *l) {
     const Choice c = choose(p, OP, a);
-    a.split = c.split, a.part = part;
+    a.split = c.split, a.part = part, l->kind = c.kind, l->part_bytes = (c.part_bytes + 255) / 256 * 256;
     return p->dtype == MOE_DT_F32 ? prepare<float, OP>(c.kind, a, l) : prepare<bf16_t, OP>(c.kind, a, l);
 }
-// The workspace: two plans, then the parts' sums of one product.
+// The workspace: two plans, then the parts' sums of a call's products.
 static FfnPlan *plans_of(void *workspace) { return (FfnPlan *)workspace; }
 static float *parts_of(void *workspace) { return (float *)((char *)workspace + (2 * sizeof(FfnPlan) + 255) / 256 * 256); }
 
@@ -153,19 +175,27 @@ static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *work
     if (rows)
         if (const int rc = prepare<OP>(p, *rows, parts, &l[0])) return rc;
     if (dw)
-        if (const int rc = prepare<kFfnDw>(p, *dw, parts, &l[1])) return rc;
+        if (const int rc = prepare<kFfnDw>(p, *dw, parts + (rows ? l[0].part_bytes / 4 : 0), &l[1])) return rc;
     FfnPlan *plans = plans_of(workspace);
     if (l[0].planned || l[1].planned) {
         FfnPlanArgs plan = {};
         if (l[0].planned) plan.rows = *rows, plan.rows_plan = plans, plan.bm = l[0].bm, rows->plan = plans;
         if (l[1].planned) plan.dw = *dw, plan.dw_plan = plans + 1, dw->plan = plans + 1;
-        hipLaunchKernelGGL(k_ffn_plan, dim3(1), dim3(kThreads), 0, st, plan);
+        hipLaunchKernelGGL(k_ffn_plan, dim3(2), dim3(kThreads), 0, st, plan);
         if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
+    }
+    const void *both = nullptr;
+    if (rows && dw) both = p->dtype == MOE_DT_F32 ? both_of<float, OP>(l[0].kind, l[1].kind) : both_of<bf16_t, OP>(l[0].kind, l[1].kind);
+    if (both) {
+        if (const int rc = allow_lds(both, l[0].smem)) return rc;
+        unsigned first = l[0].groups;
+        void *args[] = {rows, dw, &first};
+        if (hipLaunchKernel(both, dim3(l[0].groups + l[1].groups), dim3(kThreads), args, l[0].smem, st) != hipSuccess) return MOE_ERR_HIP;
     }
     for (int i = 0; i < 2; ++i) {
         if (!a[i]) continue;
         void *args[] = {a[i]};
-        if (hipLaunchKernel(l[i].kernel, dim3(l[i].groups), dim3(kThreads), args, l[i].smem, st) != hipSuccess) return MOE_ERR_HIP;
+        if (!both && hipLaunchKernel(l[i].kernel, dim3(l[i].groups), dim3(kThreads), args, l[i].smem, st) != hipSuccess) return MOE_ERR_HIP;
         if (!l[i].join) continue;
         const size_t pieces = (i ? (size_t)a[i]->E * a[i]->M * (a[i]->o1 ? 2 : 1) : (size_t)a[i]->rows) * (a[i]->N / 8), groups = (pieces + kThreads - 1) / kThreads;
         if (hipLaunchKernel(l[i].join, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(kThreads), args, 0, st) != hipSuccess) return MOE_ERR_HIP;
@@ -182,17 +212,17 @@ extern "C" {
 
 size_t moe_ffn_workspace_bytes(const moe_problem_t *p) {
     if (check_problem(p) != MOE_OK) return 0;
-    size_t parts = 0;
+    size_t parts[6];  // up, down, dh, dx, dW2, dW1 and dW3
     for (int i = 0; i < 6; ++i) {
         FfnArgs a = args_of(p, nullptr);
         const FfnOp op = (FfnOp)(i < kFfnDw ? i : kFfnDw);
-        const bool down = i == kFfnDw;  // dW2; 5: dW1 and dW3
+        const bool down = i == kFfnDw;
         a.down = down, a.M = down ? p->f : p->d, a.N = op == kFfnDw ? (down ? p->d : p->f) : op == kFfnUp || op == kFfnDh ? p->f : p->d;
         a.K = op == kFfnUp || op == kFfnDh ? p->d : p->f;
-        const size_t bytes = choose(p, op, a).part_bytes;
-        if (bytes > parts) parts = bytes;
+        parts[i] = (choose(p, op, a).part_bytes + 255) / 256 * 256;
     }
-    return (size_t)((char *)parts_of(nullptr) - (char *)nullptr) + (parts + 255) / 256 * 256;
+    const size_t down_backward = parts[kFfnDh] + parts[4], up_backward = parts[kFfnDx] + parts[5];
+    return (size_t)((char *)parts_of(nullptr) - (char *)nullptr) + std::max({parts[kFfnUp], parts[kFfnDown], down_backward, up_backward});
 }
 
 static int check_workspace(const void *ws) { return !ws || ((uintptr_t)ws & 255) != 0 ? MOE_ERR_WORKSPACE : MOE_OK; }
