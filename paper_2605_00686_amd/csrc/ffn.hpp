@@ -9,6 +9,14 @@
 //
 // All are tiles of C[m,n] = sum over k of A(m,k) B(k,n) on the matrix cores; what differs is which of an operand's indices is contiguous
 // in memory, k ("KC" below) or the other one, and what is done with a tile's sums.  Sums are fp32, outputs are rounded once.
+//
+// What bounds them: with hundreds of rows per expert the matrix cores (2 operations per multiply, 1.2 PFLOP/s of bf16 in a large product of the
+// library's on this card, whose clock falls to 1.55 GHz under that load); with dozens and fewer the weights, read once (5 to 6 TB/s).  Reached:
+// 16384 x 2 of 8 experts of 4096 x 14336 up 1.13 PFLOP/s, dx and dw 1.13 together; 128 x 8 of 128 of 2048 x 768 down 5.9 TB/s; 4096 x 8 of 128 of 2048 x
+// 768, where both take about the same, up 306 us of the 222 that its bytes take in a copy.  What is left of the matrix cores' time: a stage
+// of 256 x 256 x 32 takes 1370 cycles, 1024 of them products; the rest is its 256 fragment reads and 32 loads per wavefront, a barrier, and dx's
+// rows of 64 bytes, half a cache line each, which ask the L2 twice.  One workgroup of 4 wavefronts per CU with 128 x 128 sums each reads LDS
+// least; 8 wavefronts, two workgroups of 128 x 256, stages of 128 bytes and starts that are staggered were level or slower.
 #pragma once
 #include <type_traits>
 
@@ -38,7 +46,7 @@ struct FfnArgs {
     const struct FfnPlan *plan;  // of k_ffn_plan, NULL: every workgroup makes its own tables and takes every n-th tile
 };
 
-constexpr int kDwStart = 96;  // rows of reduction that the start and end of a tile of dw cost as much as
+constexpr int kDwStart = 96;  // rows of reduction that the start and end of a tile of dw are counted as (1 to 384: the same times within 1 %)
 
 // One operand's stage: R indices x KB bytes of the reduction (64: 32 steps of bf16, 16 of fp32), R * KB bytes of LDS.
 //   KC:     [R][KB bytes]
@@ -132,7 +140,8 @@ __device__ __forceinline__ int last_up_to(const int *list, int n, int v) {
     return uniform(found) - 1;
 }
 
-// Tiles in groups of kTileGroup rows of tiles, column by column inside a group.
+// Tiles in groups of kTileGroup rows of tiles, column by column inside a group: what an XCD works on at a time shares operands in its L2.  16384 x 2 of
+// 8 experts of 4096 x 14336 up, ms, by 1 / 2 / 4 / 8: 8.08 / 7.23 / 6.91 / 6.90; 4096 x 8 of 128 of 2048 x 768, us: 317 / 321 / 324 / 334.
 constexpr int kTileGroup = 4;
 __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r, int *c) {
     const int group = t / (kTileGroup * cols), in = t - group * kTileGroup * cols, first = group * kTileGroup;
@@ -339,7 +348,8 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     }
     const int row_blocks = uniform(tables->edge[kTileQueues]) / a.nt;  // (dw: of tiles)
     // The tile after this one.  Where there is a plan, tiles are handed out as workgroups come for them, first of the own XCD's list, then of
-    // the others': experts' last row blocks, and dw's experts, differ in what they take.
+    // the others': experts' last row blocks, and dw's experts, differ in what they take.  (Without / with a plan: 4096 x 4 of 128 of 2880 x 2880 down
+    // 607 / 560 us, 16384 x 2 of 8 of 4096 x 14336 dx and dw 14.6 / 13.6 ms.)
     int list = group % kTileQueues;
     const int mine = group / kTileQueues, per_list = groups / kTileQueues;
     int taken = 0;  // thread 0: what it was given of `list`
@@ -400,7 +410,8 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
         return w;
     };
 
-    // Row blocks that are not full have loops of their own, for a quarter, a half and three quarters of the rows, and more stages in flight.
+    // Row blocks that are not full have loops of their own, for a quarter, a half and three quarters of the rows, and more stages in flight: 0.38 us
+    // a stage for 64 rows, 0.82 for 256.
     constexpr bool SHORT = !DW && SZ == 2 && T::MB % 4 == 0;
     auto loads_of_a = [](int live) __attribute__((always_inline)) { return (OA::INSTR * live / T::MB + T::WAVES - 1) / T::WAVES; };
 
@@ -905,7 +916,8 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     ffn<T, OP>(a, blockIdx.x, gridDim.x);
 }
 // A backward call's two products in one launch: workgroups of dw take the CUs that the rows' product leaves, at its end or, where it is small, from
-// the start.  us, kernels one after the other / this: fp32 256 x 2 of 8 of 512 x 1024 dh and dW2 36 / 29, 1001 x 6 of 48 dx and dW1, dW3 228 / 197;
+// the start.  us, kernels one after the other / this: fp32 256 x 2 of 8 of 512 x 1024 dh and dW2 36 / 29, 1001 x 6 of 48 of
+// 1040 x 368 dx, dW1 and dW3 228 / 197;
 // bf16 4096 x 8 of 128 of 2048 x 768 480 / 425 and 745 / 725, 16384 x 2 of 8 of 4096 x 14336 13900 / 13600.
 template <class T, FfnOp OP, class TDW>
 __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn_both(FfnArgs a, FfnArgs dw, u32 first) {
@@ -916,7 +928,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn_both(FfnArgs a, FfnArg
         ffn<TDW, kFfnDw>(dw, blockIdx.x - first, gridDim.x - first);
 }
 
-// The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.
+// The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.  5 us, most of it the launch.
 template <typename ET, FfnOp OP>
 __global__ __launch_bounds__(kThreads) void k_ffn_join(FfnArgs a) {
     __shared__ u64 lds[8];

@@ -38,7 +38,8 @@ struct Launch {
     int kind, bm;
     bool planned;
 };
-// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us).  (Tiles of 32 rows take the same each.)
+// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us; what it gains: see k_ffn).  Tiles of 32 rows take
+// the same each: 128 x 8 of 128 of 2048 x 768 down 76 us, with a plan 81.
 constexpr int kPlannedTiles = 2;
 
 // The tiles there are to choose from, and what they take where all CUs have them: us for 64 bytes of the reduction, at the start and end, and
@@ -61,6 +62,12 @@ template <> struct TileOf<float, 0> { typedef FfnTile<float, 2, 2, 2, 2, 1, 64, 
 template <> struct TileOf<float, 1> { typedef FfnTile<float, 1, 2, 2, 2, 1, 64, 2> type; };
 
 // The tile, and the parts of the reduction, that take least by what they are worth.  (256 CUs, whatever the card: the workspace goes by it.)
+// Measured, us, * what is taken.  By tile, 256 x 256 / 128 x 128 / 32 x 256 / 32 x 128: one token of 8 of 128 of 2048 x 768 up - / 18.2 / 17.5 / 15.0*; 128 x
+// 8 down 80 / 90 / 76* / 88; 4096 x 8 up 315* / 399 / 561 / 690; 4096 x 4 of 128 of 2880 x 2880 down 561* / 673 / 929 / 968; 4096 x 8 dh and dW2, by
+// dW2's tile, 404* / 481.  fp32, 1001 x 6 of 48 of 1040 x 368, 128 rows / 64: by dx's 221 / 216*, by dw's 216* / 231.  By parts, 1 / 2 / 4 / 8 / 16 /
+// 32: a token of 2 of 8 of 4096 x 14336 down 92 / 59 / 51 / 50* / 52 / 58; 16384 rows of 2 experts of 256 x 256 dx, dW1 and dW3 122 / 87 / 64 / 53 / 50 / 55
+// (each with its own: 34*); fp32 one row of 2048 x 512 down 86 / 48 / 28 / 20* / 17 / 19; where the model errs: 64 x 2 of 8 of 1024 x 2816 dx, dW1 and
+// dW3 62 / 59 / 67 (66*).
 constexpr int kCus = 256, kMostParts = 32;
 constexpr size_t kPartBytes = (size_t)32 << 20;  // of parts' sums, at most
 // fp32: stages that the tile of 128 rows may add up in one sum (1024 steps).  Of 3584 steps the 2-norm of the error was 1.0e-6 of the result's, that of
