@@ -214,6 +214,13 @@ def moe_ffn_workspace_bytes(p: MoeProblem) -> int:
     return int(_lib.moe_ffn_workspace_bytes(ctypes.byref(p)))
 
 
+def _here(*tensors):
+    """The tensors are the current device's, which the launch goes to."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == device, "tensors of the current device"
+
+
 def _like_rows(*tensors):
     """[rows, f] tensors or views (or None) whose rows are the same number of elements apart: that number, and their addresses."""
     shape = None
@@ -253,6 +260,7 @@ def _like_matrices(*tensors):
 
 
 def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
+    _here(x_perm, W1, W3, counts, g, u, h, workspace)
     ldw, w1, w3 = _like_matrices(W1, W3)
     ld, gp, up = _like_rows(g, u)
     _check(_lib.moe_ffn_up(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, _ptr(counts), gp, up, ld, _ptr(h), _ptr(workspace),
@@ -260,17 +268,20 @@ def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
 
 
 def moe_ffn_down(p, h, W2, counts, y, workspace, stream=None):
+    _here(h, W2, counts, y, workspace)
     _check(_lib.moe_ffn_down(ctypes.byref(p), _ptr(h), _ptr(W2), _ptr(counts), _ptr(y), _ptr(workspace), _stream(stream)),
            "moe_ffn_down")
 
 
 def moe_ffn_down_backward(p, dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace, stream=None):
+    _here(dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace)
     ld, gp, up, dgp, dup = _like_rows(g, u, dg, du)
     _check(_lib.moe_ffn_down_backward(ctypes.byref(p), _ptr(dy), _ptr(W2), _ptr(h), gp, up, _ptr(counts), _ptr(dh), dgp, dup, ld,
                                       _ptr(dW2), _ptr(workspace), _stream(stream)), "moe_ffn_down_backward")
 
 
 def moe_ffn_up_backward(p, x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace, stream=None):
+    _here(x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace)
     ldw, w1, w3, dw1, dw3 = _like_matrices(W1, W3, dW1, dW3)
     ld, dgp, dup = _like_rows(dg, du)
     _check(_lib.moe_ffn_up_backward(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, dgp, dup, ld, _ptr(counts), _ptr(dx), dw1, dw3,
@@ -285,6 +296,16 @@ class TensorList:
         for i, o in zip(ins, outs):
             assert i.is_cuda and i.is_contiguous() and o.is_contiguous() and o.device == i.device, "device tensors, contiguous"
             assert i.dtype == o.dtype and i.numel() == o.numel() and i.dtype in (torch.float32, torch.bfloat16), "fp32 or bf16, both the same"
+        # (one named twice would be counted twice, and scaled by whoever comes first or by both)
+        spans = []
+        for i, o in zip(ins, outs):
+            for t in (i,) if i.data_ptr() == o.data_ptr() else (i, o):
+                if t.numel():
+                    spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+        spans.sort()
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "tensors that do not overlap"
+        assert len({t.get_device() for t in ins}) <= 1, "tensors of one device"
+        self.device = ins[0].get_device() if len(ins) else None
         self.tensors = list(ins), list(outs)
         self.n = len(self.tensors[0])
         self.array = (MoeTensor * max(1, self.n))(*(MoeTensor(i.data_ptr(), o.data_ptr(), i.numel(), MOE_DT_F32 if i.dtype == torch.float32 else MOE_DT_BF16, 0)
@@ -301,10 +322,14 @@ def moe_grad_workspace_bytes(tensors: TensorList) -> int:
 
 
 def moe_grad_norm(tensors, sum_squares, norm, workspace, stream=None):
+    assert tensors.device in (None, torch.cuda.current_device()), "tensors of the current device"
+    _here(sum_squares, norm, workspace)
     _check(_lib.moe_grad_norm(tensors.array, tensors.n, _ptr(sum_squares), _ptr(norm), _ptr(workspace), _stream(stream)), "moe_grad_norm")
 
 
 def moe_grad_clip(tensors, sum_squares, max_norm, stream=None):
+    assert tensors.device in (None, torch.cuda.current_device()), "tensors of the current device"
+    _here(sum_squares)
     _check(_lib.moe_grad_clip(tensors.array, tensors.n, _ptr(sum_squares), float(max_norm), _stream(stream)), "moe_grad_clip")
 
 

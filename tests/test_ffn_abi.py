@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2605_00686_amd import binding as B
 
@@ -140,3 +141,46 @@ def test_workspace_of_the_norm():
     assert B._lib.moe_grad_workspace_bytes(t, n) == 256
     t, n = tensors(*[(0x10000, 0x20000, 1 << 30, 1)] * 200)
     assert B._lib.moe_grad_workspace_bytes(t, n) >= 3 * 2048 * 8
+
+
+class Numbers:  # a device tensor as far as a list of tensors looks
+    is_cuda, dtype, device = True, torch.float32, "cuda:0"
+
+    def __init__(self, at, n, where=0):
+        self.at, self.n, self.where = at, n, where
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.at
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 4
+
+    def get_device(self):
+        return self.where
+
+
+def test_lists_of_tensors_that_overlap_or_lie_on_two_devices_are_refused():
+    a, b, empty = Numbers(0x1000, 64), Numbers(0x1100, 64), Numbers(0x1010, 0)
+    assert B.tensor_list([a, b, empty]).n == 3 and B.tensor_list([a], [b]).n == 1 and B.tensor_list([]).device is None
+    for ins, outs in (([a, a], None), ([a, Numbers(0x10fc, 4)], None), ([a], [Numbers(0x1004, 64)]), ([a, b], [b, Numbers(0x2000, 64)]),
+                      ([a, Numbers(0x9000, 4, where=1)], None)):
+        with pytest.raises(AssertionError):
+            B.tensor_list(ins, outs)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    here, there = Numbers(0x1000, 64, where=1), Numbers(0x1000, 64)
+    B._here(here, None, here)
+    with pytest.raises(AssertionError):
+        B._here(here, None, there)
+    for call in (lambda: B.moe_ffn_down(problem(), there, here, here, here, here), lambda: B.moe_grad_norm(B.tensor_list([there]), here, here, here),
+                 lambda: B.moe_grad_clip(B.tensor_list([there]), here, 1.0), lambda: B.moe_grad_clip(B.tensor_list([here]), there, 1.0)):
+        with pytest.raises(AssertionError):
+            call()

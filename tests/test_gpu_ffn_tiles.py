@@ -70,6 +70,63 @@ def test_captured_and_replayed(shape):
         assert all(torch.equal(out[n], want[n]) for n in out)
 
 
+@pytest.mark.parametrize("shape", MIXED, ids=ids)
+def test_no_rows(shape):
+    """No expert has any: every output is zeros, the rows' and the gradients'."""
+    gen = torch.Generator().manual_seed(27)
+    r = F.Rows(gen, *shape)
+    run, out, n = all_calls(r, gen)
+    n.zero_()
+    run()
+    assert all((t == 0).all() for t in out.values())
+
+
+@pytest.mark.parametrize("shape", [(1100, 5, 1, 192, 320, 0, "bf16"), (3, 8, 2, 1984, 192, 0, "bf16"), (200, 3, 1, 80, 208, 90, "f32"), (1636, 64, 2, 64, 448, 0, "bf16")],
+                         ids=ids)
+def test_strides_and_nothing_around_is_touched(shape):
+    """Rows and matrices further apart than they are long, 16 bytes behind a line's start: the results of dense ones, and what lies between is kept."""
+    from paper_2605_00686_amd import binding as B
+    gen = torch.Generator().manual_seed(28)
+    r = F.Rows(gen, *shape)
+    x, dy, W1, W3, W2 = r.draw(gen, r.d).cuda(), r.draw(gen, r.d).cuda(), r.weights(gen, r.d, r.f).cuda(), r.weights(gen, r.d, r.f).cuda(), r.weights(gen, r.f, r.d).cuda()
+    p, n, ws = r.problem(), r.counts.cuda(), workspace(r.problem())
+    piece = 16 // x.element_size()
+
+    def wide(rows, cols):  # rows, and a row before and behind, with 3 pieces between
+        whole = torch.full((rows + 2, cols + 3 * piece), 77.0, dtype=r.dt, device="cuda")
+        return whole, whole[1:-1, piece:piece + cols]
+
+    def matrices(t):
+        whole, view = wide(r.E * t.shape[1], t.shape[2])
+        view = view.unflatten(0, t.shape[:2])
+        view.copy_(t)
+        return whole, view
+
+    def calls(g, u, dg, du, h, y, dW2, dx, dW1, dW3, w1, w3):
+        B.moe_ffn_up(p, x, w1, w3, n, g, u, h, ws)
+        B.moe_ffn_down(p, h, W2, n, y, ws)
+        B.moe_ffn_down_backward(p, dy, W2, h, g, u, n, None, dg, du, dW2, ws)
+        B.moe_ffn_up_backward(p, x, w1, w3, dg, du, n, dx, dW1, dW3, ws)
+    dense = dict(g=(r.n, r.f), u=(r.n, r.f), dg=(r.n, r.f), du=(r.n, r.f), h=(r.n, r.f), y=(r.n, r.d), dW2=W2.shape, dx=(r.n, r.d), dW1=W1.shape, dW3=W1.shape)
+    want = {name: poisoned(*s, dt=r.dt) for name, s in dense.items()}
+    calls(**want, w1=W1, w3=W3)
+    wholes, got = {}, {}
+    for name, s in dense.items():
+        if name in ("dW1", "dW3"):
+            wholes[name], got[name] = matrices(poisoned(*s, dt=r.dt))
+        elif name in ("g", "u", "dg", "du"):
+            wholes[name], got[name] = wide(*s)
+        else:  # dense ones, 16 bytes behind a line's start and with numbers on both sides
+            size = torch.Size(s).numel()
+            wholes[name] = torch.full((size + 2 * piece,), 77.0, dtype=r.dt, device="cuda")
+            got[name] = wholes[name][piece:-piece].view(s)
+    calls(**got, w1=matrices(W1)[1], w3=matrices(W3)[1])
+    for name in dense:
+        assert torch.equal(got[name], want[name]), name
+        got[name].fill_(77.0)
+        assert (wholes[name] == 77.0).all(), name
+
+
 def test_calls_at_the_same_time():
     """Two streams, each with a workspace of its own."""
     gen = torch.Generator().manual_seed(22)
