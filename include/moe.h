@@ -365,6 +365,7 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
  *   one from 2^-110 on).  Where a sum comes out infinite or not a number, it and those up to 128 rows and columns around it are made of whole fp32
  *   numbers: numbers that are not finite, or only just, have their effect and no other, but for last places of the expert's other rows and columns.
  *   workspace: moe_ffn_workspace_bytes() bytes, 256-byte aligned, any content; calls that may run at the same time have one each.
+ *   (It holds a call's plan and the sums of reductions that are cut: a captured call keeps it as long as the graph.)  Everything lies on the current device.
  *   The calls keep nothing: the same inputs give the same bits.  A launch of 2^32 threads or more is MOE_ERR_UNSUPPORTED.
  */
 

@@ -216,7 +216,7 @@ def moe_ffn_workspace_bytes(p: MoeProblem) -> int:
 
 def _here(*tensors):
     """The tensors are the current device's, which the launch goes to."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()  # (torch.cuda.current_device() takes twice as long)
     for t in tensors:
         assert t is None or t.get_device() == device, "tensors of the current device"
 
@@ -305,7 +305,7 @@ class TensorList:
         spans.sort()
         assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "tensors that do not overlap"
         assert len({t.get_device() for t in ins}) <= 1, "tensors of one device"
-        self.device = ins[0].get_device() if len(ins) else None
+        self.one = ins[0] if len(ins) else None
         self.tensors = list(ins), list(outs)
         self.n = len(self.tensors[0])
         self.array = (MoeTensor * max(1, self.n))(*(MoeTensor(i.data_ptr(), o.data_ptr(), i.numel(), MOE_DT_F32 if i.dtype == torch.float32 else MOE_DT_BF16, 0)
@@ -322,14 +322,12 @@ def moe_grad_workspace_bytes(tensors: TensorList) -> int:
 
 
 def moe_grad_norm(tensors, sum_squares, norm, workspace, stream=None):
-    assert tensors.device in (None, torch.cuda.current_device()), "tensors of the current device"
-    _here(sum_squares, norm, workspace)
+    _here(tensors.one, sum_squares, norm, workspace)
     _check(_lib.moe_grad_norm(tensors.array, tensors.n, _ptr(sum_squares), _ptr(norm), _ptr(workspace), _stream(stream)), "moe_grad_norm")
 
 
 def moe_grad_clip(tensors, sum_squares, max_norm, stream=None):
-    assert tensors.device in (None, torch.cuda.current_device()), "tensors of the current device"
-    _here(sum_squares)
+    _here(tensors.one, sum_squares)
     _check(_lib.moe_grad_clip(tensors.array, tensors.n, _ptr(sum_squares), float(max_norm), _stream(stream)), "moe_grad_clip")
 
 
