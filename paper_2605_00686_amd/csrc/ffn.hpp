@@ -326,7 +326,7 @@ __device__ __forceinline__ Cut cut_f32(const u32x4_t &lo, const u32x4_t &hi) {
     return c;
 }
 
-// Workgroup `group` of `groups`.  (Unsigned: divisions of signed numbers here took down of 4096 x 4 of 128 of 2880 x 2880 from 580 to 700 us.)
+// Workgroup `group` of `groups`.
 template <class T, FfnOp OP>
 __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     typedef typename T::ET ET;
@@ -357,6 +357,9 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
         if (a.plan && tid == 0) taken = (int)atomicAdd(&a.plan->taken[list].v, 1u);
     };
     auto answer = [&]() __attribute__((always_inline)) {  // thread 0; the others read it behind a barrier
+        // (Waited for here by everybody, asked or not: the compiler would do so where it next needs the register, which may be in the loops below, and
+        // for all of a tile's loads in flight: 4096 x 4 of 128 of 2880 x 2880 down 580 us, so 700.)
+        asm volatile("" : "+v"(taken));
         if (!a.plan || tid) return;
         int t = tables->edge[list] + per_list + taken;
         for (int tries = 1; t >= tables->edge[list + 1] && tries < kTileQueues; ++tries) {
@@ -844,6 +847,12 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
                 }
             }
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (OP == kFfnDh) {  // (what was fetched and not used is waited for here, not among the next tile's loads)
+#pragma unroll
+            for (int at = 0; at < GU_AHEAD; ++at)
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) asm volatile("" : : "v"(gv[at][i]), "v"(uv[at][i]));
+        }
     };
 
     // The next tile's first stages are on their way while this one's results go out.
