@@ -397,9 +397,9 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
             w.row0 = r * T::BM;
             w.end = (w.s.used + STEPS - 1) / STEPS;
         } else {
-            tile_in_groups(t, row_blocks, a.nt, &r, &c);
-            const int e = last_up_to(tables->first, a.E + 1, r);
-            w.s.e = e, w.s.block = r - uniform(tables->first[e]);
+            const int e = last_up_to(tables->first, a.E + 1, t / a.nt), first = uniform(tables->first[e]);
+            tile_in_groups(t - first * a.nt, (e < a.E ? uniform(tables->first[e + 1]) : row_blocks) - first, a.nt, &r, &c);
+            w.s.e = e, w.s.block = r;
             w.s.begin = uniform(a.capacity ? e * a.capacity : tables->begin[e]);
             w.s.used = e < a.E ? uniform(tables->used[e]) : 0;
             w.s.extent = a.capacity ? a.capacity : e < a.E ? w.s.used : a.rows - w.s.begin;
