@@ -140,9 +140,10 @@ __device__ __forceinline__ int last_up_to(const int *list, int n, int v) {
     return uniform(found) - 1;
 }
 
-// Tiles in groups of kTileGroup rows of tiles, column by column inside a group: what an XCD works on at a time shares operands in its L2.  16384 x 2 of
-// 8 experts of 4096 x 14336 up, ms, by 1 / 2 / 4 / 8: 8.08 / 7.23 / 6.91 / 6.90; 4096 x 8 of 128 of 2048 x 768, us: 317 / 321 / 324 / 334.
-constexpr int kTileGroup = 4;
+// Tiles of an expert in groups of kTileGroup rows of tiles, column by column inside a group: the 32 that an XCD works on at a time share operands in its
+// L2.  16384 x 2 of 8 experts of 4096 x 14336 up, ms, by 1 / 2 / 3 / 4 / 6 / 8: 8.08 / 7.23 / 6.95 / 6.80 / 6.75 / 6.80; 4096 x 8 of 128 of 2048 x 768 the same
+// by all.  Groups that go over experts' ends: 4096 x 4 of 128 of 2880 x 2880 down 594 us, these 560.
+constexpr int kTileGroup = 6;
 __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r, int *c) {
     const int group = t / (kTileGroup * cols), in = t - group * kTileGroup * cols, first = group * kTileGroup;
     const int n = min(kTileGroup, rows - first);
