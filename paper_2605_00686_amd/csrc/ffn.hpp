@@ -14,7 +14,7 @@
 // library's on this card, whose clock falls to 1.55 GHz under that load); with dozens and fewer the weights, read once (5 to 6 TB/s).  Reached:
 // 16384 x 2 of 8 experts of 4096 x 14336 up 1.14 PFLOP/s, dx and dw 1.14 together; 128 x 8 of 128 of 2048 x 768 down 5.9 TB/s; 4096 x 8 of 128 of 2048 x
 // 768, where both take about the same, up 301 us, of which its bytes take 222 in a copy.  What is left of the matrix cores' time: a stage
-// of 256 x 256 x 32 takes 1370 cycles, 1024 of them products; the rest is its 256 fragment reads and 32 loads per wavefront, a barrier, and dx's
+// of 256 x 256 x 32 takes 1370 cycles, 1024 of them products; the rest is 24 to 40 LDS reads and 8 loads per wavefront, a barrier, and dx's
 // rows of 64 bytes, half a cache line each, which ask the L2 twice.  One workgroup of 4 wavefronts per CU with 128 x 128 sums each reads LDS
 // least; 8 wavefronts, two workgroups of 128 x 256, stages of 128 bytes and starts that are staggered were level or slower.
 #pragma once
