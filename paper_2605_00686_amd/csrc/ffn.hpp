@@ -23,6 +23,7 @@
 #include "gemm_bf16.hpp"
 #include "pieces.hpp"
 #include "swiglu8.hpp"
+#include "tile_lists.hpp"
 
 namespace moe {
 
@@ -45,8 +46,6 @@ struct FfnArgs {
     float *part;  // [split][rows][N] (up: g then u for each part); dw: [split][matrix][E][M][N]
     const struct FfnPlan *plan;  // of k_ffn_plan, NULL: every workgroup makes its own tables and takes every n-th tile
 };
-
-constexpr int kDwStart = 96;  // rows of reduction that the start and end of a tile of dw are counted as (1 to 384: the same times within 1 %)
 
 // One operand's stage: R indices x KB bytes of the reduction (64: 32 steps of bf16, 16 of fp32), R * KB bytes of LDS.
 //   KC:     [R][KB bytes]
@@ -190,15 +189,8 @@ __device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables 
     }
     __syncthreads();
     if (DW) {
-        if (tid <= kTileQueues) {
-            // stretches of about the same work: a tile is worth its expert's rows and kDwStart
-            const int per = a.mt * a.nt;
-            const u64 at = (u64)tid * (u32)total;
-            int e = 0;
-            for (int step = kMaxExperts / 2; step; step >>= 1)
-                if (e + step < a.E && t->first[e + step] <= (int)(at / kTileQueues)) e += step;
-            t->edge[tid] = tid == kTileQueues ? a.E * per : e * per + (int)((at - (u64)kTileQueues * t->first[e]) * per / (u64)(kTileQueues * (t->used[e] + kDwStart)));
-        }
+        static_assert(kDwLists == kTileQueues && kMaxExperts <= 256, "as dw_edge has them");
+        if (tid <= kTileQueues) t->edge[tid] = dw_edge(tid, a.E, a.mt * a.nt, total, t->first, t->used);
         __syncthreads();
     }
 }
