@@ -135,16 +135,23 @@ __device__ __forceinline__ double clip_factor(double sum, float max_norm) {
     const double norm = sqrt(sum);
     return norm > max_norm && norm < __builtin_inf() ? max_norm / norm : 1.0;
 }
-// fp32 in 64 bits and bf16 in 32: one rounding that counts
-__device__ __forceinline__ float scaled(float g, double factor, float) { return (float)(g * factor); }
-__device__ __forceinline__ float scaled(float g, double factor, bf16_t) { return g * (float)factor; }
+// One rounding that counts: products in 64 bits for fp32, in 32 for bf16, but for a factor below fp32's normal numbers (a norm past 2^100, say,
+// clipped to 10^-8), of which fp32 has a few bits or none where the results are numbers like any other.
+struct InFp32 {
+    float factor;
+    __device__ __forceinline__ float operator()(float g) const { return g * factor; }
+};
+struct InFp64 {
+    double factor;
+    __device__ __forceinline__ float operator()(float g) const { return (float)(g * factor); }
+};
 
 __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
     const double factor = clip_factor(*a.sum, a.max_norm);
     // (backwards: the norm has left the last numbers in the caches)
     for_each_chunk<true>(a, [&](int t, bool f32, long long first, int n) {
         if (factor == 1.0 && a.in[t] == a.out[t]) return;
-        auto chunk = [&](auto zero) {
+        auto chunk = [&](auto zero, auto scaled) {
             typedef decltype(zero) ET;
             constexpr int PER = Piece<ET>::N;
             const ET *p = (const ET *)a.in[t] + first;
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
                 float f[PER];
                 Piece<ET>::unpack(v[i], f);
 #pragma unroll
-                for (int j = 0; j < PER; ++j) f[j] = scaled(f[j], factor, zero);
+                for (int j = 0; j < PER; ++j) f[j] = scaled(f[j]);
                 const u32x4_t w = Piece<ET>::pack(f);
                 if (aligned)
                     store_past((u32x4_t *)q + k, w);
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
             }
             for (int i = 0; i < rest; ++i) {
                 const size_t at = (size_t)part * PER + i;
-                const float g = scaled(Elem<ET>::load(p, at), factor, zero);
+                const float g = scaled(Elem<ET>::load(p, at));
                 if constexpr (sizeof(ET) == 4)
                     q[at] = g;
                 else
@@ -177,9 +184,11 @@ __global__ __launch_bounds__(kThreads) void k_grad_clip(GradArgs a) {
             }
         };
         if (f32)
-            chunk(0.f);
+            chunk(0.f, InFp64{factor});
+        else if (factor >= 0x1p-126)
+            chunk(bf16_t{0}, InFp32{(float)factor});
         else
-            chunk(bf16_t{0});
+            chunk(bf16_t{0}, InFp64{factor});
     });
 }
 
