@@ -369,7 +369,8 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
  *   The calls keep nothing: the same inputs give the same bits.  A launch of 2^32 threads or more is MOE_ERR_UNSUPPORTED.
  */
 
-/* Host, pure: bytes of workspace that the four calls need, 0 if the problem is invalid. */
+/* Host, pure: bytes of workspace that the four calls need, 0 if the problem is invalid.  They are enough for every problem of the same E, d, f, dtype
+ * and layout with fewer rows too (T k, E * capacity): a program asks once, for its largest batch. */
 size_t moe_ffn_workspace_bytes(const moe_problem_t *p);
 
 /* g = x_perm W1[e], u = x_perm W3[e], h = silu(g) u (of the sums, before g and u are rounded).  g and u: both or none may be NULL; h may be

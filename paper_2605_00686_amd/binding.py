@@ -259,17 +259,23 @@ def _like_matrices(*tensors):
     return out
 
 
+def _ffn_workspace(p, workspace):
+    """Its address; the C call cannot see how long it is."""
+    assert workspace is None or workspace.nbytes >= _lib.moe_ffn_workspace_bytes(ctypes.byref(p)), "a workspace of moe_ffn_workspace_bytes()"
+    return _ptr(workspace)
+
+
 def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
     _here(x_perm, W1, W3, counts, g, u, h, workspace)
     ldw, w1, w3 = _like_matrices(W1, W3)
     ld, gp, up = _like_rows(g, u)
-    _check(_lib.moe_ffn_up(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, _ptr(counts), gp, up, ld, _ptr(h), _ptr(workspace),
+    _check(_lib.moe_ffn_up(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, _ptr(counts), gp, up, ld, _ptr(h), _ffn_workspace(p, workspace),
                            _stream(stream)), "moe_ffn_up")
 
 
 def moe_ffn_down(p, h, W2, counts, y, workspace, stream=None):
     _here(h, W2, counts, y, workspace)
-    _check(_lib.moe_ffn_down(ctypes.byref(p), _ptr(h), _ptr(W2), _ptr(counts), _ptr(y), _ptr(workspace), _stream(stream)),
+    _check(_lib.moe_ffn_down(ctypes.byref(p), _ptr(h), _ptr(W2), _ptr(counts), _ptr(y), _ffn_workspace(p, workspace), _stream(stream)),
            "moe_ffn_down")
 
 
@@ -277,7 +283,7 @@ def moe_ffn_down_backward(p, dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace
     _here(dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace)
     ld, gp, up, dgp, dup = _like_rows(g, u, dg, du)
     _check(_lib.moe_ffn_down_backward(ctypes.byref(p), _ptr(dy), _ptr(W2), _ptr(h), gp, up, _ptr(counts), _ptr(dh), dgp, dup, ld,
-                                      _ptr(dW2), _ptr(workspace), _stream(stream)), "moe_ffn_down_backward")
+                                      _ptr(dW2), _ffn_workspace(p, workspace), _stream(stream)), "moe_ffn_down_backward")
 
 
 def moe_ffn_up_backward(p, x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace, stream=None):
@@ -285,7 +291,7 @@ def moe_ffn_up_backward(p, x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspa
     ldw, w1, w3, dw1, dw3 = _like_matrices(W1, W3, dW1, dW3)
     ld, dgp, dup = _like_rows(dg, du)
     _check(_lib.moe_ffn_up_backward(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, dgp, dup, ld, _ptr(counts), _ptr(dx), dw1, dw3,
-                                    _ptr(workspace), _stream(stream)), "moe_ffn_up_backward")
+                                    _ffn_workspace(p, workspace), _stream(stream)), "moe_ffn_up_backward")
 
 
 class TensorList:
@@ -310,6 +316,7 @@ class TensorList:
         self.n = len(self.tensors[0])
         self.array = (MoeTensor * max(1, self.n))(*(MoeTensor(i.data_ptr(), o.data_ptr(), i.numel(), MOE_DT_F32 if i.dtype == torch.float32 else MOE_DT_BF16, 0)
                                                     for i, o in zip(*self.tensors)))
+        self.workspace_bytes = int(_lib.moe_grad_workspace_bytes(self.array, self.n))
 
 
 def tensor_list(ins, outs=None) -> TensorList:
@@ -318,11 +325,12 @@ def tensor_list(ins, outs=None) -> TensorList:
 
 
 def moe_grad_workspace_bytes(tensors: TensorList) -> int:
-    return int(_lib.moe_grad_workspace_bytes(tensors.array, tensors.n))
+    return tensors.workspace_bytes
 
 
 def moe_grad_norm(tensors, sum_squares, norm, workspace, stream=None):
     _here(tensors.one, sum_squares, norm, workspace)
+    assert workspace is None or workspace.nbytes >= tensors.workspace_bytes, "a workspace of moe_grad_workspace_bytes()"
     _check(_lib.moe_grad_norm(tensors.array, tensors.n, _ptr(sum_squares), _ptr(norm), _ptr(workspace), _stream(stream)), "moe_grad_norm")
 
 

@@ -74,14 +74,35 @@ constexpr size_t kPartBytes = (size_t)32 << 20;  // of parts' sums, at most
 // an fp32 product of the library's; what is longer, and dw where an expert could have more rows, is left to 64 rows and their sums of sums, 4e-7 at
 // any length, for 1.27 times the time.
 constexpr int kOneSum = 64;
+constexpr double kLeastStages = 8;                // of a part
 struct Choice {
     int kind, split;
     size_t part_bytes;
 };
+static int matrices_of(FfnOp op, const FfnArgs &a) { return op == kFfnUp || (op == kFfnDw && !a.down) ? 2 : 1; }  // (dW1 and dW3: alone as together, for the same bits)
+static double rows_per_expert(const moe_problem_t *p) {  // of one that has any, about
+    const int slots = p->T * p->k;
+    return (double)slots / (p->E < slots ? p->E : slots);
+}
+static double stages_of(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {
+    return op == kFfnDw ? rows_per_expert(p) * elem_bytes(p) / 64 : (op == kFfnDx ? 2.0 : 1.0) * a.K * elem_bytes(p) / 64;
+}
+static size_t sums_of(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {  // bytes of a part's
+    return (op == kFfnDw ? (size_t)p->E * a.M : (size_t)a.rows) * a.N * matrices_of(op, a) * 4;
+}
+// Room for the sums of whatever parts the product is cut into, with these rows or with fewer: a product of rows may be cut into more parts where there are
+// fewer rows (their tiles leave CUs idle, and their sums fit kPartBytes), and a program asks once, for the most rows it has.
+static size_t room_of(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {
+    int s = 1;
+    while (2 * s <= kMostParts && stages_of(p, op, a) / (2 * s) >= kLeastStages) s *= 2;  // (not more of them with fewer rows)
+    const size_t sums = sums_of(p, op, a);
+    if (op == kFfnDw)  // the sums are of the same size whatever the rows
+        while (s > 1 && s * sums > kPartBytes) s /= 2;
+    return s == 1 ? 0 : std::min(s * sums, kPartBytes);
+}
 static Choice choose(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {
-    const int slots = p->T * p->k, experts = p->E < slots ? p->E : slots, sz = elem_bytes(p);
-    const int mats = op == kFfnUp || (op == kFfnDw && !a.down) ? 2 : 1;  // (dW1 and dW3: alone as together, for the same bits)
-    const double rows = (double)slots / experts;  // of an expert that has any, about
+    const int slots = p->T * p->k, experts = p->E < slots ? p->E : slots, sz = elem_bytes(p), mats = matrices_of(op, a);
+    const double rows = rows_per_expert(p);
     Choice best = {0, 1, 0};
     double best_us = 0;
     for (int k = 0; k < (sz == 4 || op == kFfnDw ? 2 : kKinds); ++k) {
@@ -92,12 +113,12 @@ static Choice choose(const moe_problem_t *p, FfnOp op, const FfnArgs &a) {
         const double per_expert = rows / t.bm + 0.5 > 1 ? rows / t.bm + 0.5 : 1;
         const double blocks = op == kFfnDw ? (double)p->E * ((a.M + t.bm - 1) / t.bm) : experts * per_expert;
         const double lacks = op == kFfnDw ? 0 : floor((t.bm - rows / per_expert) / 64);
-        const double stages = op == kFfnDw ? rows * sz / 64 : (op == kFfnDx ? 2.0 : 1.0) * a.K * sz / 64;
+        const double stages = stages_of(p, op, a);
         const double longest = op == kFfnDw ? p->T * sz / 64. : stages;
         for (int s = 1; s <= kMostParts; s *= 2) {
             if (sz == 4 && k == 0 && longest / s > kOneSum) continue;
-            if (s > 1 && stages / s < 8) break;
-            const size_t bytes = s == 1 ? 0 : (size_t)s * (op == kFfnDw ? (size_t)p->E * a.M : (size_t)a.rows) * a.N * mats * 4;
+            if (s > 1 && stages / s < kLeastStages) break;
+            const size_t bytes = s == 1 ? 0 : s * sums_of(p, op, a);
             if (bytes > kPartBytes) break;
             const double per = blocks * nt * s / (kCus * t.occ), rounds = per <= 1 ? 1 : per + 0.5;
             const double us = rounds * (stages / s * (t.stage_us - lacks * t.less_us) + t.more_us) + (s > 1 ? 6 + bytes / 2e6 : 0);
@@ -226,7 +247,7 @@ size_t moe_ffn_workspace_bytes(const moe_problem_t *p) {
         const bool down = i == kFfnDw;
         a.down = down, a.M = down ? p->f : p->d, a.N = op == kFfnDw ? (down ? p->d : p->f) : op == kFfnUp || op == kFfnDh ? p->f : p->d;
         a.K = op == kFfnUp || op == kFfnDh ? p->d : p->f;
-        parts[i] = (choose(p, op, a).part_bytes + 255) / 256 * 256;
+        parts[i] = (room_of(p, op, a) + 255) / 256 * 256;
     }
     const size_t down_backward = parts[kFfnDh] + parts[4], up_backward = parts[kFfnDx] + parts[5];
     return (size_t)((char *)parts_of(nullptr) - (char *)nullptr) + std::max({parts[kFfnUp], parts[kFfnDown], down_backward, up_backward});
