@@ -259,6 +259,21 @@ def _like_matrices(*tensors):
     return out
 
 
+def _fit(p, counts, rows_d=(), rows_f=(), matrices=(), views=(), matrix_views=()):
+    """Tensors (or None) of the types that the calls read and write, and not shorter: contiguous [rows, d], [rows, f] and [E, f, d], views [rows, f]
+    and [E, d, f].  (The C calls see addresses.)"""
+    dtype, E, d, f, capacity = torch.float32 if p.dtype == MOE_DT_F32 else torch.bfloat16, p.E, p.d, p.f, p.capacity
+    assert counts is None or counts.dtype == torch.int32 and counts.numel() >= E, "counts: int32, one per expert"
+    rows = E * capacity if capacity else p.T * p.k
+    for size, tensors in ((rows * d, rows_d), (rows * f, rows_f), (E * d * f, matrices)):
+        for t in tensors:
+            assert t is None or t.dtype == dtype and t.numel() >= size, "tensors of the problem's type and size"
+    for t in views:
+        assert t is None or t.dtype == dtype and t.shape[0] >= rows and t.shape[1] == f, "rows of the problem's type and size"
+    for t in matrix_views:
+        assert t is None or t.dtype == dtype and t.shape[0] >= E and t.shape[1] == d and t.shape[2] == f, "matrices of the problem's type and size"
+
+
 def _ffn_workspace(p, workspace):
     """Its address; the C call cannot see how long it is."""
     assert workspace is None or workspace.nbytes >= _lib.moe_ffn_workspace_bytes(ctypes.byref(p)), "a workspace of moe_ffn_workspace_bytes()"
@@ -267,6 +282,7 @@ def _ffn_workspace(p, workspace):
 
 def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
     _here(x_perm, W1, W3, counts, g, u, h, workspace)
+    _fit(p, counts, (x_perm,), (h,), (), (g, u), (W1, W3))
     ldw, w1, w3 = _like_matrices(W1, W3)
     ld, gp, up = _like_rows(g, u)
     _check(_lib.moe_ffn_up(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, _ptr(counts), gp, up, ld, _ptr(h), _ffn_workspace(p, workspace),
@@ -275,12 +291,14 @@ def moe_ffn_up(p, x_perm, W1, W3, counts, g, u, h, workspace, stream=None):
 
 def moe_ffn_down(p, h, W2, counts, y, workspace, stream=None):
     _here(h, W2, counts, y, workspace)
+    _fit(p, counts, (y,), (h,), (W2,))
     _check(_lib.moe_ffn_down(ctypes.byref(p), _ptr(h), _ptr(W2), _ptr(counts), _ptr(y), _ffn_workspace(p, workspace), _stream(stream)),
            "moe_ffn_down")
 
 
 def moe_ffn_down_backward(p, dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace, stream=None):
     _here(dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace)
+    _fit(p, counts, (dy,), (h, dh), (W2, dW2), (g, u, dg, du))
     ld, gp, up, dgp, dup = _like_rows(g, u, dg, du)
     _check(_lib.moe_ffn_down_backward(ctypes.byref(p), _ptr(dy), _ptr(W2), _ptr(h), gp, up, _ptr(counts), _ptr(dh), dgp, dup, ld,
                                       _ptr(dW2), _ffn_workspace(p, workspace), _stream(stream)), "moe_ffn_down_backward")
@@ -288,6 +306,7 @@ def moe_ffn_down_backward(p, dy, W2, h, g, u, counts, dh, dg, du, dW2, workspace
 
 def moe_ffn_up_backward(p, x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace, stream=None):
     _here(x_perm, W1, W3, dg, du, counts, dx, dW1, dW3, workspace)
+    _fit(p, counts, (x_perm, dx), (), (), (dg, du), (W1, W3, dW1, dW3))
     ldw, w1, w3, dw1, dw3 = _like_matrices(W1, W3, dW1, dW3)
     ld, dgp, dup = _like_rows(dg, du)
     _check(_lib.moe_ffn_up_backward(ctypes.byref(p), _ptr(x_perm), w1, w3, ldw, dgp, dup, ld, _ptr(counts), _ptr(dx), dw1, dw3,
@@ -328,14 +347,21 @@ def moe_grad_workspace_bytes(tensors: TensorList) -> int:
     return tensors.workspace_bytes
 
 
+def _norm_fits(sum_squares, norm=None):
+    assert sum_squares is None or sum_squares.dtype == torch.float64 and sum_squares.numel(), "sum_squares: float64"
+    assert norm is None or norm.dtype == torch.float32 and norm.numel(), "norm: float32"
+
+
 def moe_grad_norm(tensors, sum_squares, norm, workspace, stream=None):
     _here(tensors.one, sum_squares, norm, workspace)
+    _norm_fits(sum_squares, norm)
     assert workspace is None or workspace.nbytes >= tensors.workspace_bytes, "a workspace of moe_grad_workspace_bytes()"
     _check(_lib.moe_grad_norm(tensors.array, tensors.n, _ptr(sum_squares), _ptr(norm), _ptr(workspace), _stream(stream)), "moe_grad_norm")
 
 
 def moe_grad_clip(tensors, sum_squares, max_norm, stream=None):
     _here(tensors.one, sum_squares)
+    _norm_fits(sum_squares)
     _check(_lib.moe_grad_clip(tensors.array, tensors.n, _ptr(sum_squares), float(max_norm), _stream(stream)), "moe_grad_clip")
 
 
