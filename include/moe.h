@@ -361,9 +361,10 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
  *   a call, W1, W3 and their gradients [E, d, f] with `ldw` elements from one row to the next and d * ldw from one expert to the next (f, or
  *   2f where the two are the halves of one [E, d, 2f]); W2, dW2 [E, f, d].  ld, ldw: >= f, whole multiples of 16 bytes; tensors start on 16 bytes.
  *   Sums are fp32, and what is made of them before an output's one rounding is too.  Outputs may not overlap inputs except where it says so.
- *   fp32 numbers are multiplied as three bf16 numbers each, off by 2^-26 of a product; of a number the bits from 2^-133 on count (all there are in
- *   one from 2^-110 on).  Where a sum comes out infinite or not a number, it and those up to 128 rows and columns around it are made of whole fp32
- *   numbers: numbers that are not finite, or only just, have their effect and no other, but for last places of the expert's other rows and columns.
+ *   fp32 numbers are multiplied as three bf16 numbers each, which hold all their bits, subnormal numbers' too; what is left out of a product is at
+ *   most 2^-24 of it.  Where a sum comes to 2^80 or more, or out infinite or not a number, or has an operand of 2^104 or more, it and those up to 128
+ *   rows and columns around it are made of whole fp32 numbers, in twice the time: numbers that are not finite, or only just, have their effect and
+ *   no other, but for last places of the expert's other rows and columns.
  *   workspace: moe_ffn_workspace_bytes() bytes, 256-byte aligned, any content; calls that may run at the same time have one each.
  *   (It holds a call's plan and the sums of reductions that are cut: a captured call keeps it as long as the graph.)  Everything lies on the current device.
  *   The calls keep nothing: the same inputs give the same bits.  A launch of 2^32 threads or more is MOE_ERR_UNSUPPORTED.

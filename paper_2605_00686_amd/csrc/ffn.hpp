@@ -297,10 +297,13 @@ __device__ __forceinline__ void multiply(const u32x4_t &b, const u32x4_t &a, f32
     }
 }
 
-// Eight fp32 numbers as three bf16 numbers each, x = p0 + p1 + p2 with |p1| <= 2^-9 |x| and |p2| <= 2^-18 |x|, off by 2^-27 |x| at most.  Of
-// the nine products of two numbers the six largest are taken; the others come to 2^-26 of the whole.  On the matrix cores those six take 192 cycles
-// for 32 x 32 x 16, the fp32 instructions 512.  A number that is not finite, or that bf16 rounds to one, makes a NaN of every sum that it is in; a
-// product that only the rounded numbers' is out of range makes it infinite.
+// Eight fp32 numbers as three bf16 numbers each: 2^24 x = p0 + p1 + p2 with |p1| and |p2| up to 2^-8 and 2^-17 of that, and nothing left, since at that
+// scale every bit that an fp32 number can have is one of a normal bf16 number.  (As they are, numbers below 2^-110 would lose bits and those
+// below 2^-133 all of them, whatever they are multiplied by; the scaling costs 1 to 4 % of a call.)  Of the nine products of two numbers the six
+// largest are taken; the others come to 2^-24 of the whole at most, half a step of fp32.  On the matrix cores those six take 192 cycles for 32 x 32
+// x 16, the fp32 instructions 512.  Sums are 2^48 times as large until their tile's end: a number of 2^104 and more, or one that is not finite,
+// and a sum of 2^80 and more come out infinite or as NaN.
+constexpr float kCutScale = 0x1p24f;
 struct Cut {
     u32x4_t part[3];
 };
@@ -308,7 +311,7 @@ __device__ __forceinline__ Cut cut_f32(const u32x4_t &lo, const u32x4_t &hi) {
     Cut c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float x = __uint_as_float(i < 2 ? lo[2 * i] : hi[2 * i - 4]), y = __uint_as_float(i < 2 ? lo[2 * i + 1] : hi[2 * i - 3]);
+        float x = __uint_as_float(i < 2 ? lo[2 * i] : hi[2 * i - 4]) * kCutScale, y = __uint_as_float(i < 2 ? lo[2 * i + 1] : hi[2 * i - 3]) * kCutScale;
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
             const u32 p = pack_bf16x2(x, y);
@@ -656,6 +659,10 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
                 if (ASK) ask();
                 multiply_cut();
             }
+#pragma unroll
+            for (int mb = 0; mb < LIVE; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb) acc[mb][nb] *= 1.f / (kCutScale * kCutScale);
         } else {
             read(stage, 0, f0);
             first_steps(std::false_type{});
@@ -890,7 +897,7 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
             } else {
                 run(std::integral_constant<int, T::MB>{});
             }
-            if constexpr (SZ == 4) {  // again on the fp32 instructions where a sum is not finite: bf16 may have rounded numbers, or their product, out of range
+            if constexpr (SZ == 4) {  // again on the fp32 instructions where a sum is not finite: numbers or sums may have been scaled out of range
                 bool bad = false;
 #pragma unroll
                 for (int mb = 0; mb < T::MB; ++mb)

@@ -71,8 +71,8 @@ template <> struct TileOf<float, 1> { typedef FfnTile<float, 1, 2, 2, 2, 1, 64, 
 constexpr int kCus = 256, kMostParts = 32;
 constexpr size_t kPartBytes = (size_t)32 << 20;  // of parts' sums, at most
 // fp32: stages that the tile of 128 rows may add up in one sum (1024 steps).  Of 3584 steps the 2-norm of the error was 1.0e-6 of the result's, that of
-// an fp32 product of the library's; what is longer, and dw where an expert could have more rows, is left to 64 rows and their sums of sums, 4e-7 at
-// any length, for 1.27 times the time.
+// an fp32 product of the library's; what is longer, and dw where an expert could have more rows, is left to 64 rows and their sums of sums, 4e-7 of
+// 16384 steps (growing with the root of their number), for 1.27 times the time.
 constexpr int kOneSum = 64;
 constexpr double kLeastStages = 8;                // of a part
 struct Choice {
