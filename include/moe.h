@@ -367,7 +367,7 @@ int moe_swiglu_backward(const moe_problem_t *p, const void *dh, const uint8_t *c
  *   no other, but for last places of the expert's other rows and columns.
  *   workspace: moe_ffn_workspace_bytes() bytes, 256-byte aligned, any content; calls that may run at the same time have one each.
  *   (It holds a call's plan and the sums of reductions that are cut: a captured call keeps it as long as the graph.)  Everything lies on the current device.
- *   The calls keep nothing: the same inputs give the same bits.  A launch of 2^32 threads or more is MOE_ERR_UNSUPPORTED.
+ *   The calls keep nothing: the same inputs give the same bits.  A product of 2^30 tiles or more (of 32 x 64 numbers at least) is MOE_ERR_UNSUPPORTED.
  */
 
 /* Host, pure: bytes of workspace that the four calls need, 0 if the problem is invalid.  They are enough for every problem of the same E, d, f, dtype
