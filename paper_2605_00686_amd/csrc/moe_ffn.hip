@@ -144,7 +144,6 @@ static int prepare(FfnArgs &a, Launch *l) {
     if (blocks * a.nt >= (size_t)1 << 30) return MOE_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
-    if (const int rc = allow_lds((const void *)k_ffn<T, OP>, T::SMEM)) return rc;
     const size_t tiles = (blocks * a.nt + kTileQueues - 1) / kTileQueues * kTileQueues, room = (size_t)cus * T::OCC;
     l->kernel = (const void *)k_ffn<T, OP>;
     l->join = a.split > 1 ? (const void *)k_ffn_join<typename T::ET, OP> : nullptr;
@@ -204,6 +203,11 @@ static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *work
         if (const int rc = prepare<OP>(p, *rows, parts, &l[0])) return rc;
     if (dw)
         if (const int rc = prepare<kFfnDw>(p, *dw, parts + (rows ? l[0].part_bytes / 4 : 0), &l[1])) return rc;
+    const void *both = nullptr;
+    if (rows && dw) both = p->dtype == MOE_DT_F32 ? both_of<float, OP>(l[0].kind, l[1].kind) : both_of<bf16_t, OP>(l[0].kind, l[1].kind);
+    for (int i = 0; i < 2; ++i)
+        if (a[i])
+            if (const int rc = allow_lds(both ? both : l[i].kernel, l[i].smem)) return rc;
     FfnPlan *plans = plans_of(workspace);
     if (l[0].planned || l[1].planned) {
         FfnPlanArgs plan = {};
@@ -212,10 +216,7 @@ static int launch(const moe_problem_t *p, FfnArgs *rows, FfnArgs *dw, void *work
         hipLaunchKernelGGL(k_ffn_plan, dim3(2), dim3(kThreads), 0, st, plan);
         if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
     }
-    const void *both = nullptr;
-    if (rows && dw) both = p->dtype == MOE_DT_F32 ? both_of<float, OP>(l[0].kind, l[1].kind) : both_of<bf16_t, OP>(l[0].kind, l[1].kind);
     if (both) {
-        if (const int rc = allow_lds(both, l[0].smem)) return rc;
         unsigned first = l[0].groups;
         void *args[] = {rows, dw, &first};
         if (hipLaunchKernel(both, dim3(l[0].groups + l[1].groups), dim3(kThreads), args, l[0].smem, st) != hipSuccess) return MOE_ERR_HIP;

@@ -10,6 +10,7 @@
 #include "common.hpp"
 #include "dispatch.hpp"
 #include "expert.hpp"
+#include "limit_memo.hpp"
 #include "problem.hpp"
 #include "route.hpp"
 
@@ -790,26 +791,15 @@ static int hip_ok(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 static int set_smem_raw(const void *kernel, size_t bytes) {
     if (bytes > 160 * 1024) return MOE_ERR_UNSUPPORTED;
     if (bytes <= 48 * 1024) return MOE_OK;
-    struct Entry {
-        int dev;
-        const void *kernel;
-        size_t limit;
-    };
     static std::mutex lock;
-    static Entry table[64];
-    static int n = 0;
+    static LimitMemo memo;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return MOE_ERR_HIP;
     std::lock_guard<std::mutex> g(lock);
-    Entry *hit = nullptr;
-    for (int i = 0; i < n; ++i)
-        if (table[i].dev == dev && table[i].kernel == kernel) hit = &table[i];
-    if (hit && hit->limit >= bytes) return MOE_OK;
+    size_t *limit = memo.of(dev, kernel);
+    if (limit && *limit >= bytes) return MOE_OK;
     if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return MOE_ERR_HIP;
-    if (hit)
-        hit->limit = bytes;
-    else if (n < 64)
-        table[n++] = Entry{dev, kernel, bytes};
+    if (limit) *limit = bytes;
     return MOE_OK;
 }
 int allow_lds(const void *kernel, size_t bytes) { return set_smem_raw(kernel, bytes); }
