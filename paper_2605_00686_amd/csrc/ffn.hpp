@@ -12,11 +12,14 @@
 //
 // What bounds them: with hundreds of rows per expert the matrix cores (2 operations per multiply, 1.2 PFLOP/s of bf16 in a large product of the
 // library's on this card, whose clock falls to 1.55 GHz under that load); with dozens and fewer the weights, read once (5 to 6 TB/s).  Reached:
-// 16384 x 2 of 8 experts of 4096 x 14336 up 1.14 PFLOP/s, dx and dw 1.14 together; 128 x 8 of 128 of 2048 x 768 down 5.9 TB/s; 4096 x 8 of 128 of 2048 x
-// 768, where both take about the same, up 301 us, of which its bytes take 222 in a copy.  What is left of the matrix cores' time: a stage
-// of 256 x 256 x 32 takes 1370 cycles, 1024 of them products; the rest is 24 to 40 LDS reads and 8 loads per wavefront, a barrier, and dx's
+// 16384 x 2 of 8 experts of 4096 x 14336 up 1.15 PFLOP/s, dx and dw 1.14 together; 128 x 8 of 128 of 2048 x 768 down 5.9 TB/s; 4096 x 8 of 128 of 2048 x
+// 768, where both take about the same, up 300 us, of which its bytes take 222 in a copy.  What is left of the matrix cores' time: a stage
+// of 256 x 256 x 32 takes 1400 cycles, 1024 of them products; the rest is 24 to 40 LDS reads and 8 loads per wavefront, a barrier, and dx's
 // rows of 64 bytes, half a cache line each, which ask the L2 twice.  One workgroup of 4 wavefronts per CU with 128 x 128 sums each reads LDS
 // least; 8 wavefronts, two workgroups of 128 x 256, stages of 128 bytes and starts that are staggered were level or slower.
+//
+// Figures here and of the choices in moe_ffn.hip are of one build: calls one after another in a graph, with two sets of inputs in turn, median on one card
+// ("kernel": of a kernel trace).  The same case is 2 % away on another card or day, and a row of calls from a program up to 6 %.
 #pragma once
 #include <type_traits>
 
@@ -140,8 +143,8 @@ __device__ __forceinline__ int last_up_to(const int *list, int n, int v) {
 }
 
 // Tiles of an expert in groups of kTileGroup rows of tiles, column by column inside a group: the 32 that an XCD works on at a time share operands in its
-// L2.  16384 x 2 of 8 experts of 4096 x 14336 up, ms, by 1 / 2 / 3 / 4 / 6 / 8: 8.08 / 7.23 / 6.95 / 6.80 / 6.75 / 6.80; 4096 x 8 of 128 of 2048 x 768 the same
-// by all.  Groups that go over experts' ends: 4096 x 4 of 128 of 2880 x 2880 down 594 us, these 560.
+// L2.  16384 x 2 of 8 experts of 4096 x 14336 up, ms, by 1 / 2 / 3 / 4 / 6 / 8: 8.05 / 7.11 / 6.90 / 6.74 / 6.67 / 6.74; 4096 x 8 of 128 of 2048 x 768 the same
+// by all.  Groups that go over experts' ends took 6 % longer for 4096 x 4 of 128 of 2880 x 2880 down.
 constexpr int kTileGroup = 6;
 __device__ __forceinline__ void tile_in_groups(int t, int rows, int cols, int *r, int *c) {
     const int group = t / (kTileGroup * cols), in = t - group * kTileGroup * cols, first = group * kTileGroup;
@@ -196,9 +199,9 @@ __device__ __forceinline__ void make_tables(const FfnArgs &a, int bm, FfnTables 
 }
 
 // dw: a plan deals the experts out to the XCDs by their rows, from the largest to the smallest and back again, and each XCD begins with its largest.
-// (For fewer experts, stretches of the same work are more even.)  us, in the experts' order / by rows: 4096 x 8 of 128 of 2048 x 768 dW2 233 / 219,
-// dW1 and dW3 418 / 404.  The products of rows stay in the experts' order: their short tiles, which wait for weights, side by side at the end
-// take longer than mixed with the others, up 329 / 351, dx 341 / 361.
+// (For fewer experts, stretches of the same work are more even.)  us, in the experts' order / by rows: 4096 x 8 of 128 of 2048 x 768 dW2 217 / 210,
+// dW1 and dW3 400 / 390.  The products of rows stay in the experts' order: their short tiles, which wait for weights, side by side at the end
+// take longer than mixed with the others, by 7 % (up) and 6 % (dx).
 constexpr int kDealtExperts = 32;
 __device__ __forceinline__ void deal_experts(const FfnArgs &a, FfnTables *t) {
     const int tid = threadIdx.x, mine = tid < a.E ? t->used[tid] : 0;
@@ -345,7 +348,7 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     const int row_blocks = uniform(tables->edge[kTileQueues]) / a.nt;  // (dw: of tiles)
     // The tile after this one.  Where there is a plan, tiles are handed out as workgroups come for them, first of the own XCD's list, then of
     // the others': experts' last row blocks, and dw's experts, differ in what they take.  (Without / with a plan: 4096 x 4 of 128 of 2880 x 2880 down
-    // 607 / 560 us, 16384 x 2 of 8 of 4096 x 14336 dx and dw 14.6 / 13.6 ms.)
+    // 568 / 530 us, 16384 x 2 of 8 of 4096 x 14336 dx and dw 14.5 / 13.6 ms.)
     int list = group % kTileQueues;
     const int mine = group / kTileQueues, per_list = groups / kTileQueues;
     int taken = 0;  // thread 0: what it was given of `list`
@@ -354,7 +357,7 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     };
     auto answer = [&]() __attribute__((always_inline)) {  // thread 0; the others read it behind a barrier
         // (Waited for here by everybody, asked or not: the compiler would do so where it next needs the register, which may be in the loops below, and
-        // for all of a tile's loads in flight: 4096 x 4 of 128 of 2880 x 2880 down 580 us, so 700.)
+        // for all of a tile's loads in flight: a fifth more time for 4096 x 4 of 128 of 2880 x 2880 down.)
         asm volatile("" : "+v"(taken));
         if (!a.plan || tid) return;
         int t = tables->edge[list] + per_list + taken;
@@ -410,7 +413,7 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
     };
 
     // Row blocks that are not full have loops of their own, for a quarter, a half and three quarters of the rows, and more stages in flight: 0.38 us
-    // a stage for 64 rows, 0.82 for 256.
+    // a stage for 64 rows, 0.82 for 256 (16384 rows x 2048 x 2048 on 8 experts, kernel).
     constexpr bool SHORT = !DW && SZ == 2 && T::MB % 4 == 0;
     auto loads_of_a = [](int live) __attribute__((always_inline)) { return (OA::INSTR * live / T::MB + T::WAVES - 1) / T::WAVES; };
 
@@ -466,8 +469,8 @@ __device__ __forceinline__ void ffn(const FfnArgs &a, u32 group, u32 groups) {
         end_stage();
     };
     // The first stages of a tile: nobody may be reading the stages any more.  up: dealt out among the blocks of the last tile's results, of which it has
-    // three times as many bytes as down.  All first / dealt out, 4096 x 8 of 128 of 2048 x 768 up 333 / 325 us, with this for all its gradients
-    // 722 / 722, 16384 x 2 of 8 of 4096 x 14336 up 6750 / 6727, its gradients 13600 / 13670.
+    // three times as many bytes as down.  All first / dealt out, us: 4096 x 8 of 128 of 2048 x 768 up 310 / 307, 16384 x 2 of 8 of 4096 x 14336 up
+    // 6735 / 6670; dealt out for the gradients too, kernel, 722 / 722 and 13600 / 13670.
     constexpr bool DEAL = GATED && T::KW == 1;
     int until = 0;  // the stage behind them
     auto start = [&](const Tile &w) __attribute__((always_inline)) {
@@ -941,9 +944,9 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn(FfnArgs a) {
     ffn<T, OP>(a, blockIdx.x, gridDim.x);
 }
 // A backward call's two products in one launch: workgroups of dw take the CUs that the rows' product leaves, at its end or, where it is small, from
-// the start.  us, kernels one after the other / this: fp32 256 x 2 of 8 of 512 x 1024 dh and dW2 36 / 29, 1001 x 6 of 48 of
-// 1040 x 368 dx, dW1 and dW3 228 / 197;
-// bf16 4096 x 8 of 128 of 2048 x 768 480 / 425 and 745 / 725, 16384 x 2 of 8 of 4096 x 14336 13900 / 13600.
+// the start.  us, kernels one after the other / this: fp32 256 x 2 of 8 of 512 x 1024 dg, du and dW2 44 / 36, 1001 x 6 of 48 of
+// 1040 x 368 dx, dW1 and dW3 232 / 217;
+// bf16 4096 x 8 of 128 of 2048 x 768 458 / 405 and 698 / 672, 16384 x 2 of 8 of 4096 x 14336 13880 / 13600.
 template <class T, FfnOp OP, class TDW>
 __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn_both(FfnArgs a, FfnArgs dw, u32 first) {
     static_assert(T::OCC == TDW::OCC && T::SMEM == TDW::SMEM, "room");
@@ -953,7 +956,7 @@ __global__ __launch_bounds__(kThreads, T::OCC) void k_ffn_both(FfnArgs a, FfnArg
         ffn<TDW, kFfnDw>(dw, blockIdx.x - first, gridDim.x - first);
 }
 
-// The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.  5 us, most of it the launch.
+// The outputs of a product whose reduction was cut: the parts' sums added in order, 8 columns a thread.  5.5 us (kernel), most of it the launch.
 template <typename ET, FfnOp OP>
 __global__ __launch_bounds__(kThreads) void k_ffn_join(FfnArgs a) {
     __shared__ u64 lds[8];

@@ -5,8 +5,8 @@
 // A square of an fp32 number is exact in 64 bits and inside its range, so nothing overflows or vanishes before the root.  Bound by memory: every
 // number is read for the norm, and read and written for the scaling; the conversions and fused products in 64 bits are a third of what the
 // vector ALU could do meanwhile.  Tensors are cut into chunks that the workgroups go through in turn, sums are added in a fixed order.
-// 1.2e9 bf16 numbers: norm 396 us (6.1 TB/s), scaling 908 (5.3 TB/s of reads and writes; from the first number on
-// instead of from the last one back 923).  120 tensors of 8 to 32768 numbers: 5 + 2 + 6 us, launches and the latency of one chunk.
+// 1.2e9 bf16 numbers, calls in a row: norm 396 us (6.1 TB/s), scaling 908 (5.3 TB/s of reads and writes; from the first number on
+// instead of from the last one back 923).  120 tensors of 8 to 32768 numbers: kernels of 5 + 2 + 6 us, launches and the latency of one chunk.
 #pragma once
 #include "pieces.hpp"
 

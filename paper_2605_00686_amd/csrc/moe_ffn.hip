@@ -38,14 +38,14 @@ struct Launch {
     int kind, bm;
     bool planned;
 };
-// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us; what it gains: see k_ffn).  Tiles of 32 rows take
-// the same each: 128 x 8 of 128 of 2048 x 768 down 76 us, with a plan 81.
+// Tiles per workgroup from which on they are handed out by a plan, which is a launch of its own (5 us; what it gains: see ffn()).  Tiles of 32 rows take
+// the same each: 128 x 8 of 128 of 2048 x 768 down 73 us, with a plan 76.
 constexpr int kPlannedTiles = 2;
 
 // The tiles there are to choose from, and what they take where all CUs have them: us for 64 bytes of the reduction, at the start and end, and
 // (256 rows) for 64 rows that a block lacks.  Measured, 16384 rows x 2048 x 2048 on 8 experts, 1.55 to 1.75 GHz: bf16 256 x 256 0.80 us a stage with
 // 256 rows, 0.38 with 64; 128 x 128, two of them per CU, 0.55; 32 x 256 0.26 and 32 x 128 0.14 (more where the weights come from memory:
-// 128 tokens x 8 of 128 of 2048 x 768 0.47); fp32 128 x 128 1.58, 64 x 128 1.02.
+// 128 tokens x 8 of 128 of 2048 x 768 0.47); fp32 128 x 128 1.58, 64 x 128 1.02 (and 4 % more since numbers are scaled as they are cut, in both).
 struct Kind {
     int bm, bn, occ;
     double stage_us, more_us, less_us;
@@ -61,18 +61,18 @@ template <> struct TileOf<bf16_t, 3> { typedef FfnTile<bf16_t, 1, 2, 1, 2, 2, 12
 template <> struct TileOf<float, 0> { typedef FfnTile<float, 2, 2, 2, 2, 1, 64, 2> type; };
 template <> struct TileOf<float, 1> { typedef FfnTile<float, 1, 2, 2, 2, 1, 64, 2> type; };
 
-// The tile, and the parts of the reduction, that take least by what they are worth.  (256 CUs, whatever the card: the workspace goes by it.)
-// Measured, us, * what is taken.  By tile, 256 x 256 / 128 x 128 / 32 x 256 / 32 x 128: one token of 8 of 128 of 2048 x 768 up - / 18.2 / 17.5 / 15.0*; 128 x
-// 8 down 80 / 90 / 76* / 88; 4096 x 8 up 315* / 399 / 561 / 690; 4096 x 4 of 128 of 2880 x 2880 down 561* / 673 / 929 / 968; 4096 x 8 dh and dW2, by
-// dW2's tile, 404* / 481.  fp32, 1001 x 6 of 48 of 1040 x 368, 128 rows / 64: by dx's 221 / 216*, by dw's 216* / 231.  By parts, 1 / 2 / 4 / 8 / 16 /
-// 32: a token of 2 of 8 of 4096 x 14336 down 92 / 59 / 51 / 50* / 52 / 58; 16384 rows of 2 experts of 256 x 256 dx, dW1 and dW3 122 / 87 / 64 / 53 / 50 / 55
-// (each with its own: 34*); fp32 one row of 2048 x 512 down 86 / 48 / 28 / 20* / 17 / 19; where the model errs: 64 x 2 of 8 of 1024 x 2816 dx, dW1 and
-// dW3 62 / 59 / 67 (66*).
+// The tile, and the parts of the reduction, that take least by what they are worth.  (256 CUs, whatever the card, for the same bits.)
+// Measured, us, * what is taken.  By tile, 256 x 256 / 128 x 128 / 32 x 256 / 32 x 128: one token of 8 of 128 of 2048 x 768 up - / 18.6 / 19.2 / 14.4*; 128 x
+// 8 down 80 / 82 / 73* / 82; 4096 x 8 up 306* / 390 / 536 / 667; 4096 x 4 of 128 of 2880 x 2880 down 530* / 624 / 817 / 907; 4096 x 8 dh and dW2, by
+// dW2's tile, 403* / 483.  fp32, 1001 x 6 of 48 of 1040 x 368, 128 rows / 64: by dx's 219 / 215*, by dw's 217* / 233.  By parts, 1 / 2 / 4 / 8 / 16 /
+// 32: a token of 2 of 8 of 4096 x 14336 down 91 / 58 / 52* / 52 / 56 / 69; 16384 rows of 2 experts of 256 x 256 dx, dW1 and dW3, by dw's, 121 / 74 / 48 / 37 / 34* /
+// 43; fp32 one row of 2048 x 512 down 91 / 51 / 30 / 21 / 18* / 19; where the model errs: 64 x 2 of 8 of 1024 x 2816 dx, dW1 and dW3, by dx's, 61 / 59 /
+// 67*.
 constexpr int kCus = 256, kMostParts = 32;
 constexpr size_t kPartBytes = (size_t)32 << 20;  // of parts' sums, at most
 // fp32: stages that the tile of 128 rows may add up in one sum (1024 steps).  Of 3584 steps the 2-norm of the error was 1.0e-6 of the result's, that of
 // an fp32 product of the library's; what is longer, and dw where an expert could have more rows, is left to 64 rows and their sums of sums, 4e-7 of
-// 16384 steps (growing with the root of their number), for 1.27 times the time.
+// 16384 steps (growing with the root of their number), for 1.25 times the time.
 constexpr int kOneSum = 64;
 constexpr double kLeastStages = 8;                // of a part
 struct Choice {
